@@ -47,7 +47,8 @@ typedef enum {
   CONQUR_ERR_NONFINITE_INPUT = -7,  /* a row of X held NaN/Inf (that row was skipped) */
   CONQUR_ERR_TIMEOUT = -8,          /* a bounded device-side wait expired */
   CONQUR_ERR_CUDA = -9,
-  CONQUR_ERR_UNSUPPORTED = -10
+  CONQUR_ERR_UNSUPPORTED = -10,
+  CONQUR_ERR_BAD_INDEX = -11        /* a cache slot, page or row range read on the device lies outside its buffer (that access was left out) */
 } conqur_status;
 
 enum { CONQUR_F32 = 0, CONQUR_BF16 = 1 };            /* storage type of X */
@@ -467,6 +468,90 @@ enum { CONQUR_HADAMARD_CUDA_CORES_ONLY = 1 };   /* flags: never take the tensor-
 int conqur_hadamard_rows(const void* X_dev, int32_t in_dtype, int64_t n, int32_t d, int64_t ldx, void* Y_dev,
                          int32_t out_dtype, int64_t ldy, int32_t flags, void* cuda_stream);
 int conqur_hadamard_status(void* cuda_stream);
+
+/*
+ * Position rotation of query and key heads, alone or after a per-head RMS norm, with the online rotation R_3 of
+ * Appendix A ("post-RoPE") in the same pass.  A head row x of head_dim elements at position p becomes
+ *   norm (conqur_norm_rope_heads only)   x <- w * x / sqrt(mean(x^2) + eps), w one weight per element, shared by the heads
+ *   rotation   pairs (a, b) of the first rotary_dim elements:  a' = m (a cos t - b sin t),  b' = m (a sin t + b cos t),
+ *              t = p f_i for pair i; pairs are (i, i + rotary_dim/2) (CONQUR_ROPE_HALF) or (2i, 2i+1) (CONQUR_ROPE_INTERLEAVED);
+ *              the other elements stay
+ *   R_3        x <- x H / sqrt(head_dim) with CONQUR_HEADS_HADAMARD (H as in conqur_hadamard_rows)
+ * CONQUR_HEADS_INVERSE (conqur_rope_heads) applies the transposed map, R_3 first and the angles negated (the amplitude m is not
+ * inverted): the backward pass of the forward call, and for m = 1 its inverse.
+ * Arithmetic is fp32, rounded once to the storage type; angles are formed in 64-bit fixed point (turns modulo 1, exact
+ * products), so that they stay accurate at any int64 position.
+ */
+enum { CONQUR_ROPE_HALF = 0, CONQUR_ROPE_INTERLEAVED = 1 };
+/* frequencies f_i = theta^(-2i/rotary_dim), i < rotary_dim/2, and how a context longer than the trained one rescales them:
+ *   NONE; LINEAR  f_i / factor; NTK  theta * factor^(r/(r-2)) in place of theta (r = rotary_dim > 2);
+ *   BANDS  a pair making u = original f_i / 2 pi turns over the trained context keeps f_i for u >= high, takes f_i / factor for
+ *          u <= low and a blend linear in u between;
+ *   RAMP   f_i (1 - g_i) + f_i / factor g_i, g_i = clamp((i - a)/(b - a), 0, 1), a = max(floor(D(high)), 0),
+ *          b = min(ceil(D(low)), r - 1), D(u) = r ln(original / 2 pi u) / (2 ln theta) (b - a at least 0.001); the amplitude m is
+ *          1 + 0.1 ln(factor); it is 1 elsewhere */
+enum { CONQUR_ROPE_SCALE_NONE = 0, CONQUR_ROPE_SCALE_LINEAR = 1, CONQUR_ROPE_SCALE_NTK = 2, CONQUR_ROPE_SCALE_BANDS = 3,
+       CONQUR_ROPE_SCALE_RAMP = 4 };
+typedef struct {
+  uint32_t struct_size;     /* = sizeof(conqur_rope_config) */
+  int32_t  rotary_dim;      /* even, 2 .. 512 */
+  int32_t  scaling;         /* CONQUR_ROPE_SCALE_* */
+  int32_t  reserved;        /* 0 */
+  double   theta;           /* > 1 */
+  double   factor;          /* >= 1 where the scaling uses it */
+  double   low, high;       /* BANDS, RAMP: 0 < low < high, turns over the trained context */
+  int64_t  original;        /* BANDS, RAMP: trained context, > 0 */
+} conqur_rope_config;
+
+/* Host only: rotary_dim/2 angular frequencies and the amplitude m. */
+int conqur_rope_frequencies(const conqur_rope_config* cfg, double* freq_out, double* amplitude_out);
+/* Bytes of the device table below (8 per pair and 8 for the amplitude); 0 on invalid arguments. */
+size_t conqur_rope_table_bytes(const conqur_rope_config* cfg);
+/* Enqueue the writing of the table (device, 8-byte aligned, caller-owned) that the calls below take.  Not synchronised. */
+int conqur_rope_table(const conqur_rope_config* cfg, void* table_dev, void* cuda_stream);
+
+/* A tensor of heads: element e of head h of token t of sequence b is data_dev[b batch_stride + t token_stride + h head_stride + e].
+ * Any strides (a slice of a fused projection, heads before tokens, 0 for an input shared by heads, tokens or sequences); an output's may not be 0.
+ * Rows on 16-byte boundaries of head_dim 64, 80, 96, 112, 128, 192 or 256 go 16 bytes at a time, others element by element. */
+typedef struct {
+  void*    data_dev;
+  int64_t  batch_stride, token_stride, head_stride;   /* elements */
+} conqur_heads;
+
+enum { CONQUR_HEADS_HADAMARD = 1, CONQUR_HEADS_INVERSE = 2 };
+typedef struct {
+  uint32_t struct_size;     /* = sizeof(conqur_heads_call) */
+  int32_t  dtype;           /* CONQUR_F32 | CONQUR_BF16: heads in and out */
+  int32_t  head_dim;        /* 1 .. 512; a power of two >= 4 with CONQUR_HEADS_HADAMARD */
+  int32_t  rotary_dim;      /* that of the table, <= head_dim; 0: no rotation (positions and table unused) */
+  int32_t  layout;          /* CONQUR_ROPE_HALF | CONQUR_ROPE_INTERLEAVED */
+  int32_t  flags;           /* CONQUR_HEADS_* */
+  int32_t  weight_dtype;    /* of the norm weights */
+  float    eps;             /* > 0, norm calls */
+  int32_t  q_heads, k_heads;/* k_heads 0: the k_* members are unused */
+  int64_t  batch, tokens;   /* batch x tokens rows per head */
+  const int64_t* positions_dev;          /* position of token t of sequence b at [b positions_batch_stride + t] */
+  int64_t  positions_batch_stride;       /* 0: every sequence has the same */
+  const void* table_dev;    /* from conqur_rope_table */
+  conqur_heads q_in, k_in, q_out, k_out; /* an output may be its own input (same data and strides), else must not overlap an input */
+  const void* q_weight_dev; /* norm calls: head_dim weights of weight_dtype; NULL = ones */
+  const void* k_weight_dev;
+  /* backward only: q_in / k_in are the FORWARD call's inputs, q_grad / k_grad the gradients of its outputs; q_out / k_out receive
+   * the gradients of the inputs (may be q_grad / k_grad), and, where not NULL, dq_weight / dk_weight those of the weights */
+  conqur_heads q_grad, k_grad;
+  float*   dq_weight_dev;   /* device fp32, head_dim: summed over heads and tokens, overwritten */
+  float*   dk_weight_dev;
+} conqur_heads_call;
+
+/* Enqueued on the stream; not synchronised.  Invalid arguments return CONQUR_ERR_INVALID_ARG and do nothing; no tokens: a no-op
+ * (the backward call then writes zeros to the weight gradients). */
+int conqur_rope_heads(const conqur_heads_call* call, void* cuda_stream);
+int conqur_norm_rope_heads(const conqur_heads_call* call, void* cuda_stream);
+/* Backward pass of conqur_norm_rope_heads (same flags and members as the forward call; CONQUR_HEADS_INVERSE is refused).  The weight gradients are
+ * summed in an order fixed by the sizes and the device: the same call gives the same bits.
+ *   scratch_dev   device, 256-byte aligned, >= conqur_norm_rope_backward_scratch_bytes(head_dim) bytes; free to reuse once the work has run */
+size_t conqur_norm_rope_backward_scratch_bytes(int32_t head_dim);
+int conqur_norm_rope_heads_backward(const conqur_heads_call* call, void* scratch_dev, size_t scratch_bytes, void* cuda_stream);
 
 const char* conqur_strerror(int status);
 

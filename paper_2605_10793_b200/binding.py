@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Tuple
 
 import numpy as np
@@ -22,6 +23,10 @@ CONQUR_QUANT_SYMMETRIC, CONQUR_QUANT_ZEROPOINT = 0, 1
 CONQUR_FOLD_INPUT, CONQUR_FOLD_OUTPUT = 0, 1
 CONQUR_DEBUG_CANARIES, CONQUR_DEBUG_SINGLE_CTA, CONQUR_DEBUG_NO_GRAPH = 1, 2, 4
 CONQUR_HADAMARD_CUDA_CORES_ONLY = 1
+CONQUR_ROPE_HALF, CONQUR_ROPE_INTERLEAVED = 0, 1
+ROPE_LAYOUTS = {"half": CONQUR_ROPE_HALF, "interleaved": CONQUR_ROPE_INTERLEAVED}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "ramp": 4}
+CONQUR_HEADS_HADAMARD, CONQUR_HEADS_INVERSE = 1, 2
 
 # Test support: when set, every Context is created with guard bands around its workspace regions, registers itself
 # here, and has them checked when it is closed; damaged bands are collected in CANARY_FAILURES.
@@ -35,6 +40,8 @@ EXPORTS = [
     "conqur_set_M", "conqur_debug_get_signs", "conqur_debug_capture_signs", "conqur_get_stats", "conqur_debug_check_canaries", "conqur_debug_trace_heads", "conqur_plan_schedule", "conqur_debug_gemm",
     "conqur_set_profiling", "conqur_get_profile", "conqur_objective_noalloc", "conqur_debug_wait_timeout", "conqur_debug_lose_wait",
     "conqur_get_diagnostics", "conqur_fold_scratch_bytes", "conqur_fold_weight", "conqur_hadamard_rows", "conqur_hadamard_status",
+    "conqur_rope_frequencies", "conqur_rope_table_bytes", "conqur_rope_table", "conqur_rope_heads", "conqur_norm_rope_heads",
+    "conqur_norm_rope_backward_scratch_bytes", "conqur_norm_rope_heads_backward",
     "conqur_strerror",
 ]
 
@@ -71,6 +78,17 @@ class conqur_profile(C.Structure):
         ("timed_launches", C.c_int64 * 8), ("flops", C.c_double * 8), ("ms", C.c_double * 8),
         ("total_launches", C.c_int64),
     ]
+
+
+class conqur_rope_config(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("rotary_dim", C.c_int32), ("scaling", C.c_int32), ("reserved", C.c_int32),
+        ("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("original", C.c_int64),
+    ]
+
+
+# conqur_heads_call, packed in one go (its members lie back to back): see include/conqur.h
+_HEADS_CALL = struct.Struct("=IiiiiiifiiqqQqQ" + 4 * "Qqqq" + "QQ" + 2 * "Qqqq" + "QQ")
 
 
 KERNEL_CLASSES = ["rownorm", "rotate_target", "accumulate", "ns_residual", "ns_poly", "ns_next", "other", "unused"]
@@ -152,6 +170,20 @@ def load() -> C.CDLL:
     lib.conqur_hadamard_rows.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, i32, vp]
     lib.conqur_hadamard_status.restype = C.c_int
     lib.conqur_hadamard_status.argtypes = [vp]
+    lib.conqur_rope_frequencies.restype = C.c_int
+    lib.conqur_rope_frequencies.argtypes = [C.POINTER(conqur_rope_config), vp, C.POINTER(C.c_double)]
+    lib.conqur_rope_table_bytes.restype = C.c_size_t
+    lib.conqur_rope_table_bytes.argtypes = [C.POINTER(conqur_rope_config)]
+    lib.conqur_rope_table.restype = C.c_int
+    lib.conqur_rope_table.argtypes = [C.POINTER(conqur_rope_config), vp, vp]
+    lib.conqur_rope_heads.restype = C.c_int
+    lib.conqur_rope_heads.argtypes = [C.c_char_p, vp]
+    lib.conqur_norm_rope_heads.restype = C.c_int
+    lib.conqur_norm_rope_heads.argtypes = [C.c_char_p, vp]
+    lib.conqur_norm_rope_backward_scratch_bytes.restype = C.c_size_t
+    lib.conqur_norm_rope_backward_scratch_bytes.argtypes = [i32]
+    lib.conqur_norm_rope_heads_backward.restype = C.c_int
+    lib.conqur_norm_rope_heads_backward.argtypes = [C.c_char_p, vp, C.c_size_t, vp]
     lib.conqur_strerror.restype = C.c_char_p
     lib.conqur_strerror.argtypes = [C.c_int]
     _lib = lib
@@ -350,6 +382,164 @@ def conqur_hadamard_status() -> int:
     """Synchronise the current stream; status of the transform kernels run since the last call (0 = ok)."""
     import torch
     return int(load().conqur_hadamard_status(torch.cuda.current_stream().cuda_stream))
+
+
+# ---- query and key heads: position rotation, per-head norms, R_3 ---------------------------------
+
+_torch = None
+
+
+def _here(x) -> int:
+    """Handle of the current stream; the tensor has to live on the current device."""
+    global _torch, _DTYPES
+    if _torch is None:
+        import torch
+        _torch = torch
+        _DTYPES = {torch.float32: CONQUR_F32, torch.bfloat16: CONQUR_BF16}
+    dev = _torch.cuda.current_device()
+    assert x.is_cuda and x.get_device() == dev, "tensors have to live on the current CUDA device"
+    return _torch._C._cuda_getCurrentRawStream(dev)
+
+
+_DTYPES: dict = {}                                # torch dtype -> C code (torch is imported on first use)
+
+
+def rope_config(rotary_dim: int, theta=10000.0, scaling="none", factor=1.0, low=0.0, high=0.0, original=0) -> conqur_rope_config:
+    return conqur_rope_config(C.sizeof(conqur_rope_config), rotary_dim, ROPE_SCALINGS[scaling], 0, theta, factor, low, high, original)
+
+
+def conqur_rope_frequencies(cfg: conqur_rope_config) -> Tuple[np.ndarray, float]:
+    """(rotary_dim/2 angular frequencies, amplitude) of a position rotation; host only."""
+    f, amp = np.zeros(max(1, cfg.rotary_dim // 2)), C.c_double()
+    rc = load().conqur_rope_frequencies(C.byref(cfg), f.ctypes.data, C.byref(amp))
+    if rc != 0:
+        raise ConqurError(rc, "conqur_rope_frequencies")
+    return f, amp.value
+
+
+class Rope:
+    """A position rotation: its frequency table in device memory.  Made once for a model, on the current device and stream.
+
+    rotary_dim: how many elements of a head rotate.  layout: "half" pairs element i with i + rotary_dim/2, "interleaved" 2i with 2i+1.
+    scaling: "none" | "linear" | "ntk" | "bands" | "ramp" with its factor, low, high and original (see include/conqur.h)."""
+
+    def __init__(self, rotary_dim: int, theta: float = 10000.0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                 low: float = 0.0, high: float = 0.0, original: int = 0):
+        import torch
+        self.cfg = rope_config(int(rotary_dim), theta, scaling, factor, low, high, original)
+        self.rotary_dim, self.layout = int(rotary_dim), ROPE_LAYOUTS[layout]
+        nbytes = load().conqur_rope_table_bytes(C.byref(self.cfg))
+        if nbytes == 0:
+            raise ConqurError(-1, "conqur_rope_table_bytes")
+        self.table = torch.empty(nbytes // 8, dtype=torch.int64, device="cuda")
+        rc = load().conqur_rope_table(C.byref(self.cfg), self.table.data_ptr(), _here(self.table))
+        if rc != 0:
+            raise ConqurError(rc, "conqur_rope_table")
+        self._ptr = self.table.data_ptr()
+
+    def frequencies(self) -> Tuple[np.ndarray, float]:
+        return conqur_rope_frequencies(self.cfg)
+
+
+_NO_HEADS = (0, 0, 0, 0)
+
+
+def _heads(x, like=None):
+    """(data, batch stride, token stride, head stride) of a (tokens, heads, d) or (batch, tokens, heads, d) tensor."""
+    assert like is None or (x.dtype == like.dtype and x.shape == like.shape and x.is_cuda and x.get_device() == like.get_device())
+    st = x.stride()
+    assert st[-1] == 1 or x.shape[-1] == 1, "the elements of a head have to lie back to back"
+    return (x.data_ptr(), 0, st[0], st[1]) if len(st) == 3 else (x.data_ptr(), st[0], st[1], st[2])
+
+
+def _heads_call(q, k, positions, rope, flags, eps, q_weight, k_weight, q_out, k_out, q_grad=None, k_grad=None, dq_weight=0, dk_weight=0):
+    shape = q.shape
+    assert len(shape) in (3, 4) and q.dtype in _DTYPES
+    batch, tokens = (1, shape[0]) if len(shape) == 3 else (shape[0], shape[1])
+    d, device = shape[-1], q.get_device()
+    k_heads = 0
+    if k is not None:
+        assert k.dtype == q.dtype and k.get_device() == device and k.dim() == q.dim() and k.shape[:-2] == shape[:-2] and k.shape[-1] == d
+        k_heads = k.shape[-2]
+    pos = pos_b = table = rotary = layout = 0
+    if rope is not None:
+        assert positions.dtype == _torch.int64 and positions.get_device() == device and rope.table.get_device() == device
+        if positions.dim() == 1:
+            assert positions.shape[0] == tokens and (positions.stride(0) == 1 or tokens <= 1)
+        else:
+            assert positions.shape == (batch, tokens) and (positions.stride(1) == 1 or tokens <= 1)
+            pos_b = positions.stride(0)
+        pos, table, rotary, layout = positions.data_ptr(), rope._ptr, rope.rotary_dim, rope.layout
+    wq = wk = wt = 0
+    for w in (q_weight, k_weight):
+        if w is not None:
+            assert w.get_device() == device and w.shape == (d,) and w.is_contiguous() and w.dtype in _DTYPES
+    if q_weight is not None:
+        wq, wt = q_weight.data_ptr(), _DTYPES[q_weight.dtype]
+    if k_weight is not None:
+        assert q_weight is None or k_weight.dtype == q_weight.dtype
+        wk, wt = k_weight.data_ptr(), _DTYPES[k_weight.dtype]
+    return _HEADS_CALL.pack(
+        _HEADS_CALL.size, _DTYPES[q.dtype], d, rotary, layout, flags, wt, eps, shape[-2], k_heads, batch, tokens, pos, pos_b, table,
+        *_heads(q), *(_NO_HEADS if k is None else _heads(k)), *_heads(q_out, q), *(_NO_HEADS if k is None else _heads(k_out, k)), wq, wk,
+        *(_NO_HEADS if q_grad is None else _heads(q_grad, q)), *(_NO_HEADS if k_grad is None else _heads(k_grad, k)), dq_weight, dk_weight)
+
+
+def _outputs(q, k, out):
+    if out is None:
+        return _torch.empty(q.shape, dtype=q.dtype, device=q.device), None if k is None else _torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    return out
+
+
+def conqur_rope_heads(q, k, positions, rope: Optional[Rope], hadamard=False, inverse=False, out=None):
+    """Position rotation of query and key heads, then R_3 if `hadamard`; `inverse`: the transposed map, which is the backward pass
+    (see include/conqur.h).
+
+    q, k: fp32 / bf16 CUDA tensors (tokens, heads, d) or (batch, tokens, heads, d), any strides but the last; k may be None.
+    positions: int64 (tokens,) or (batch, tokens).  out: (q_out, k_out), which may be (q, k).  Returns (q_out, k_out)."""
+    stream = _here(q)
+    q_out, k_out = _outputs(q, k, out)
+    flags = (CONQUR_HEADS_HADAMARD if hadamard else 0) | (CONQUR_HEADS_INVERSE if inverse else 0)
+    rc = (_lib or load()).conqur_rope_heads(_heads_call(q, k, positions, rope, flags, 0.0, None, None, q_out, k_out), stream)
+    if rc != 0:
+        raise ConqurError(rc, "conqur_rope_heads")
+    return q_out, k_out
+
+
+def conqur_norm_rope_heads(q, k, q_weight, k_weight, positions, rope: Optional[Rope], eps=1e-6, hadamard=False, out=None):
+    """RMS norm of every head row with a weight per element (None = ones), then conqur_rope_heads, in one pass (rope None: no rotation)."""
+    stream = _here(q)
+    q_out, k_out = _outputs(q, k, out)
+    call = _heads_call(q, k, positions, rope, CONQUR_HEADS_HADAMARD if hadamard else 0, eps, q_weight, k_weight, q_out, k_out)
+    rc = (_lib or load()).conqur_norm_rope_heads(call, stream)
+    if rc != 0:
+        raise ConqurError(rc, "conqur_norm_rope_heads")
+    return q_out, k_out
+
+
+def conqur_norm_rope_heads_backward(q_grad, k_grad, q, k, q_weight, k_weight, positions, rope: Optional[Rope], eps=1e-6, hadamard=False,
+                                    out=None, scratch=None):
+    """Backward pass of conqur_norm_rope_heads: from the gradients of its outputs and its inputs, (dq, dk, dq_weight, dk_weight); the
+    weights' are fp32 (d,), summed over tokens and heads.  scratch: a 256-byte aligned uint8 tensor of
+    conqur_norm_rope_backward_scratch_bytes(d) to use instead of a new one."""
+    stream = _here(q)
+    lib = _lib or load()
+    d = q.shape[-1]
+    need = lib.conqur_norm_rope_backward_scratch_bytes(d)
+    if need == 0:
+        raise ConqurError(-1, "conqur_norm_rope_backward_scratch_bytes")
+    assert q_grad is not None and (k is None) == (k_grad is None)
+    if scratch is None:
+        scratch = _torch.empty(need, dtype=_torch.uint8, device=q.device)
+    assert scratch.dtype == _torch.uint8 and scratch.is_contiguous() and scratch.get_device() == q.get_device()
+    dq, dk = _outputs(q, k, out)
+    dw = _torch.empty((2, d), dtype=_torch.float32, device=q.device)
+    call = _heads_call(q, k, positions, rope, CONQUR_HEADS_HADAMARD if hadamard else 0, eps, q_weight, k_weight, dq, dk, q_grad, k_grad,
+                       dw.data_ptr(), 0 if k is None else dw.data_ptr() + 4 * d)
+    rc = lib.conqur_norm_rope_heads_backward(call, scratch.data_ptr(), scratch.numel(), stream)
+    if rc != 0:
+        raise ConqurError(rc, "conqur_norm_rope_heads_backward")
+    return dq, dk, dw[0], None if k is None else dw[1]
 
 
 # ---- convenience wrapper: owns the workspace tensor, checks status codes ------------------------

@@ -1530,6 +1530,7 @@ extern "C" const char* conqur_strerror(int s) {
     case CONQUR_ERR_TIMEOUT: return "bounded device-side wait expired";
     case CONQUR_ERR_CUDA: return "CUDA error";
     case CONQUR_ERR_UNSUPPORTED: return "unsupported configuration";
+    case CONQUR_ERR_BAD_INDEX: return "index outside its buffer (access left out)";
     default: return "unknown status";
   }
 }

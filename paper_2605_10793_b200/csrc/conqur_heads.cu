@@ -1,0 +1,805 @@
+// Query and key heads on their way into attention: position rotation (conqur_rope_heads), per-head RMS norm with the rotation
+// (conqur_norm_rope_heads) and its backward pass, each with the online rotation R_3 of Appendix A in the same pass.
+//
+// All of them read every head row once and write it once; 2 (bf16) or 4 bytes each way an element against some 10 to 20
+// instructions, so memory sets the pace and what has to be kept small is the work per element:
+//   - A warp takes one token and walks its heads: the rotation's angles depend on the token and the pair alone, so each lane forms the eight
+//     cosines and sines its elements need once and keeps them in registers over all heads.
+//   - A head row of D elements lies in D/16 lanes, two 16-byte (bf16) pieces each, chosen so that both elements of every pair are in
+//     one lane: no exchange for the rotation, log2(D/16) exchanges for the norm's sum and for R_3 (log2 16 of its levels are
+//     inside a lane).
+//   - Angles: the table holds each frequency in turns per position as a 64-bit binary fraction.  position * fraction modulo 2^64 is the
+//     exact turn modulo 1 (one 64-bit product, no range reduction, any position), its top 32 bits go to sincospif.
+// Rows that do not fit that scheme (head_dim not a multiple of 16 or without an instance below, half-layout pairs that do not lie in
+// whole pieces, rows off 16-byte boundaries) take a kernel that keeps one row per warp in shared memory.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cmath>
+
+#include "../../include/conqur.h"
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+struct HeadsPtr {
+  const void* in;
+  void* out;
+  const void* grad;
+  int64_t in_b, in_t, in_h, out_b, out_t, out_h, grad_b, grad_t, grad_h;
+  const void* weight;
+  int heads;
+};
+
+struct HeadsArgs {
+  HeadsPtr seg[2];                 // queries, keys
+  int64_t n, tokens;               // rows per head in all, per sequence
+  const int64_t* pos;
+  int64_t pos_b;
+  const unsigned long long* table;
+  float* partial;                  // backward: one row of head_dim sums per block
+  float eps, scale;                // scale: 1 / sqrt(head_dim), R_3
+  int head_dim, rot, layout, hadamard, inverse, weight_bf16;
+  int q_blocks;                    // backward: blocks [0, q_blocks) work on the queries, the others on the keys
+};
+
+enum { MODE_ROPE = 0, MODE_NORM = 1, MODE_GRAD = 2 };
+constexpr int HEADS_THREADS = 128;
+constexpr int HEADS_WARPS = HEADS_THREADS / 32;
+constexpr int GRAD_BLOCKS_MAX = 1184;      // 8 per SM: rows of partial weight gradients in the scratch
+
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// Eight consecutive elements, as 16-byte pieces.
+template <typename T> struct Piece;
+template <> struct Piece<bf16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float* x) const {
+    x[0] = lo_f(v.x); x[1] = hi_f(v.x); x[2] = lo_f(v.y); x[3] = hi_f(v.y);
+    x[4] = lo_f(v.z); x[5] = hi_f(v.z); x[6] = lo_f(v.w); x[7] = hi_f(v.w);
+  }
+  static __device__ __forceinline__ void store(bf16* p, const float* x) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+  }
+};
+template <> struct Piece<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + 4);
+  }
+  __device__ __forceinline__ void get(float* x) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float* x) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  }
+};
+
+__device__ __forceinline__ float load1(const bf16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ void store1(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ float load_weight(const void* w, int bf, int i) {
+  if (!w) return 1.f;
+  return bf ? __bfloat162float(static_cast<const bf16*>(w)[i]) : static_cast<const float*>(w)[i];
+}
+
+// cos and sin of 2 pi * (position * turns mod 1).  The signed top half of the 64-bit product is the turn in [-1/2, 1/2) to 2^-32;
+// rounded to fp32 it is off by at most 2^-26 of a turn.
+__device__ __forceinline__ void angle(unsigned long long pos, unsigned long long turns, float amp, float& c, float& s) {
+  const float x = (float)(int)(uint32_t)((pos * turns) >> 32) * 4.656612873077393e-10f;   // 2^-31: in half turns
+  sincospif(x, &s, &c);
+  c *= amp;
+  s *= amp;
+}
+
+// Sum over a row's L consecutive lanes; every lane gets it.  `l`: the lane's place in its row.
+template <int L>
+__device__ __forceinline__ float row_sum(float v, int l, int lane) {
+  if ((L & (L - 1)) == 0) {
+#pragma unroll
+    for (int m = 1; m < L; m <<= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    return v;
+  }
+  constexpr int P = L > 16 ? 16 : L > 8 ? 8 : L > 4 ? 4 : L > 2 ? 2 : 1;   // largest power of two below L
+#pragma unroll
+  for (int m = P; m >= 1; m >>= 1) {
+    const float o = __shfl_down_sync(0xffffffffu, v, m);
+    if (l < m && l + m < L) v += o;
+  }
+  return __shfl_sync(0xffffffffu, v, lane - l);
+}
+
+// One row (or the matching one of the gradients), spread over D/16 lanes.
+template <int D>
+struct Row {
+  static constexpr int L = D / 16;                 // lanes a row takes
+  static constexpr int PER_WARP = 32 / L;          // rows a warp works on side by side
+};
+
+template <int L>
+__device__ __forceinline__ void row_hadamard(float (&x)[16], int l, float scale) {
+#pragma unroll
+  for (int m = 1; m < 16; m <<= 1)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (!(i & m)) {
+        const float a = x[i], b = x[i | m];
+        x[i] = a + b;
+        x[i | m] = a - b;
+      }
+#pragma unroll
+  for (int m = 1; m < L; m <<= 1) {
+    const float sgn = (l & m) ? -1.f : 1.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = fmaf(sgn, x[i], __shfl_xor_sync(0xffffffffu, x[i], m));
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] *= scale;
+}
+
+// Pairs whose bit in `turned` is clear stay as they are.
+__device__ __forceinline__ void row_rotate(float (&x)[16], const float (&c)[8], const float (&s)[8], float sign, int layout, uint32_t turned) {
+  if (layout == CONQUR_ROPE_HALF) {
+    if (turned) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float a = x[i], b = x[8 + i], t = sign * s[i];
+        x[i] = fmaf(a, c[i], -b * t);
+        x[8 + i] = fmaf(a, t, b * c[i]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float a = x[2 * i], b = x[2 * i + 1], t = sign * s[i];
+      if (turned & (1u << i)) {
+        x[2 * i] = fmaf(a, c[i], -b * t);
+        x[2 * i + 1] = fmaf(a, t, b * c[i]);
+      }
+    }
+  }
+}
+
+// A lane's two pieces of a row and the eight rotations they need.
+struct LanePlan {
+  int p0, p1;                       // first elements of the two pieces
+  uint32_t turned;                  // which of its eight pairs rotate
+  int f[2];                         // frequency of pair i < 4: f[0] + i, i >= 4: f[1] + i - 4
+};
+template <int D>
+__device__ __forceinline__ LanePlan lane_plan(int l, int rot, int layout) {
+  constexpr int L = D / 16;
+  LanePlan q;
+  if (layout == CONQUR_ROPE_HALF && rot > 0) {
+    const int rp = rot >> 4;                                  // piece i of the first half pairs with piece i + rp
+    int c0;
+    if ((D & (D - 1)) == 0 && (rp & (rp - 1)) == 0) {         // a bit of the piece index becomes the register bit, for R_3
+      const int b = 31 - __clz(rp);
+      c0 = ((l >> b) << (b + 1)) | (l & (rp - 1));
+      q.p1 = 8 * (c0 + rp);
+    } else {
+      c0 = l < rp ? l : 2 * rp + 2 * (l - rp);
+      q.p1 = 8 * (l < rp ? l + rp : c0 + 1);
+    }
+    q.p0 = 8 * c0;
+    q.turned = c0 < rp ? 0xFFu : 0u;
+    q.f[0] = q.p0;
+    q.f[1] = q.p0 + 4;
+  } else {
+    q.p0 = 8 * l;
+    q.p1 = 8 * (l + L);
+    q.f[0] = q.p0 >> 1;
+    q.f[1] = q.p1 >> 1;
+    q.turned = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (2 * (q.f[i >> 2] + (i & 3)) < rot) q.turned |= 1u << i;
+  }
+  return q;
+}
+
+__device__ __forceinline__ void token_of(const HeadsArgs& a, int64_t t, int64_t& b, int64_t& s) {
+  b = 0;
+  s = t;
+  if (a.tokens != a.n) {
+    b = t / a.tokens;
+    s = t - b * a.tokens;
+  }
+}
+
+__device__ __forceinline__ void lane_angles(const HeadsArgs& a, int64_t b, int64_t t, const LanePlan& q, float (&c)[8], float (&s)[8]) {
+  if (!q.turned) return;
+  const unsigned long long pos = (unsigned long long)a.pos[b * a.pos_b + t];
+  const float amp = (float)__longlong_as_double((long long)a.table[a.rot >> 1]);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (q.turned & (1u << i)) angle(pos, a.table[q.f[i >> 2] + (i & 3)], amp, c[i], s[i]);
+}
+
+// Forward (and conqur_rope_heads' inverse).  Warp w of block x works on token HEADS_WARPS x + w; block row y of gridDim.y takes every gridDim.y-th group of
+// Row<D>::PER_WARP heads (more than one only where the tokens alone would leave the GPU idle).
+template <typename T, int D, bool NORM>
+__global__ void __launch_bounds__(HEADS_THREADS) heads_kernel(const HeadsArgs a) {
+  constexpr int L = Row<D>::L, PW = Row<D>::PER_WARP;
+  const int lane = threadIdx.x & 31;
+  const int row = lane / L, l = lane - row * L;
+  const int64_t token = (int64_t)blockIdx.x * HEADS_WARPS + (threadIdx.x >> 5);
+  if (token >= a.n) return;
+  int64_t b, t;
+  token_of(a, token, b, t);
+  const LanePlan q = lane_plan<D>(l, a.rot, a.layout);
+  const int nq = (a.seg[0].heads + PW - 1) / PW, total = nq + (a.seg[1].heads + PW - 1) / PW;
+
+  auto source = [&](int it, const T*& p) -> bool {
+    const HeadsPtr& g = a.seg[it >= nq];
+    const int h = (it >= nq ? it - nq : it) * PW + row;
+    p = static_cast<const T*>(g.in) + b * g.in_b + t * g.in_t + h * g.in_h;
+    return row < PW && h < g.heads;
+  };
+  Piece<T> r0, r1;
+  const T* p;
+  int it = blockIdx.y;
+  if (source(it, p)) {
+    r0.load(p + q.p0);
+    r1.load(p + q.p1);
+  }
+  float c[8], s[8];
+  lane_angles(a, b, t, q, c, s);
+  const float sign = a.inverse ? -1.f : 1.f;
+  float w[NORM ? 16 : 1];
+  int have = -1;
+  for (; it < total; it += gridDim.y) {
+    const int sg = it >= nq;
+    float x[16];
+    r0.get(x);
+    r1.get(x + 8);
+    const int next = it + gridDim.y;
+    if (next < total && source(next, p)) {                    // the next rows travel while these are worked on
+      r0.load(p + q.p0);
+      r1.load(p + q.p1);
+    }
+    if (NORM) {
+      if (have != sg) {
+        have = sg;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = load_weight(a.seg[sg].weight, a.weight_bf16, (i < 8 ? q.p0 : q.p1) + (i & 7));
+      }
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+      ss = row_sum<L>(ss, l, lane);
+      const float rstd = 1.f / sqrtf(ss * (1.f / D) + a.eps);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] *= rstd * w[i];
+    }
+    if (!NORM && a.inverse && a.hadamard) row_hadamard<L>(x, l, a.scale);
+    row_rotate(x, c, s, sign, a.layout, q.turned);
+    if (!(!NORM && a.inverse) && a.hadamard) row_hadamard<L>(x, l, a.scale);
+    const HeadsPtr& g = a.seg[sg];
+    const int h = (sg ? it - nq : it) * PW + row;
+    if (row < PW && h < g.heads) {
+      T* o = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + h * g.out_h;
+      Piece<T>::store(o + q.p0, x);
+      Piece<T>::store(o + q.p1, x + 8);
+    }
+  }
+}
+
+// Backward of the normed form.  With g = the gradient taken back through R_3 and the rotation, r = 1 / sqrt(mean x^2 + eps):
+//   dw = sum over rows of g * x r        dx = r (w g - x r^2 mean(w g x))
+// A block works on the queries or on the keys; its warps walk tokens and keep their share of dw in registers.
+template <typename T, int D>
+__global__ void __launch_bounds__(HEADS_THREADS) heads_grad_kernel(const HeadsArgs a) {
+  constexpr int L = Row<D>::L, PW = Row<D>::PER_WARP;
+  __shared__ float sums[HEADS_WARPS][D];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row = lane / L, l = lane - row * L;
+  const int sg = (int)blockIdx.x >= a.q_blocks;
+  const int blk = sg ? blockIdx.x - a.q_blocks : blockIdx.x, blocks = sg ? gridDim.x - a.q_blocks : a.q_blocks;
+  const HeadsPtr& g = a.seg[sg];
+  const LanePlan q = lane_plan<D>(l, a.rot, a.layout);
+  const int total = (g.heads + PW - 1) / PW;
+  float w[16], dw[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    w[i] = load_weight(g.weight, a.weight_bf16, (i < 8 ? q.p0 : q.p1) + (i & 7));
+    dw[i] = 0.f;
+  }
+  for (int64_t token = (int64_t)blk * HEADS_WARPS + warp; token < a.n; token += (int64_t)blocks * HEADS_WARPS) {
+    int64_t b, t;
+    token_of(a, token, b, t);
+    const T* xp = static_cast<const T*>(g.in) + b * g.in_b + t * g.in_t + row * g.in_h;
+    const T* yp = static_cast<const T*>(g.grad) + b * g.grad_b + t * g.grad_t + row * g.grad_h;
+    T* op = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + row * g.out_h;
+    Piece<T> x0, x1, y0, y1;
+    bool mine = row < PW && row < g.heads;
+    auto fetch = [&](int it) {
+      x0.load(xp + it * PW * g.in_h + q.p0);
+      x1.load(xp + it * PW * g.in_h + q.p1);
+      y0.load(yp + it * PW * g.grad_h + q.p0);
+      y1.load(yp + it * PW * g.grad_h + q.p1);
+    };
+    if (mine) fetch(0);
+    float c[8], s[8];
+    lane_angles(a, b, t, q, c, s);
+    for (int it = 0; it < total; ++it) {
+      float x[16], y[16];
+      x0.get(x); x1.get(x + 8);
+      y0.get(y); y1.get(y + 8);
+      const bool now = mine;
+      mine = row < PW && (it + 1) * PW + row < g.heads;
+      if (it + 1 < total && mine) fetch(it + 1);
+      if (a.hadamard) row_hadamard<L>(y, l, a.scale);
+      row_rotate(y, c, s, -1.f, a.layout, q.turned);
+      float ss = 0.f, sx = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        ss = fmaf(x[i], x[i], ss);
+        sx = fmaf(w[i] * y[i], x[i], sx);
+      }
+      ss = row_sum<L>(ss, l, lane);
+      sx = row_sum<L>(sx, l, lane);
+      const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
+      const float k = sx * (1.f / D) * r * r;
+      if (now) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float u = x[i] * r;
+          dw[i] = fmaf(y[i], u, dw[i]);
+          y[i] = r * fmaf(w[i], y[i], -x[i] * k);
+        }
+        Piece<T>::store(op + it * PW * g.out_h + q.p0, y);
+        Piece<T>::store(op + it * PW * g.out_h + q.p1, y + 8);
+      }
+    }
+  }
+  // rows of the warp, then warps of the block, in a fixed order
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float v = dw[i];
+#pragma unroll
+    for (int j = 1; j < PW; ++j) {
+      const float o = __shfl_sync(0xffffffffu, dw[i], (j * L + l) & 31);
+      v += o;
+    }
+    if (row == 0) sums[warp][(i < 8 ? q.p0 : q.p1) + (i & 7)] = v;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < D; e += HEADS_THREADS) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < HEADS_WARPS; ++k) v += sums[k][e];
+    a.partial[(int64_t)blockIdx.x * D + e] = v;
+  }
+}
+
+// Weight gradients from the blocks' rows: 32 columns and 32 shares of the rows a block, summed in a fixed order.
+__global__ void __launch_bounds__(1024) heads_weight_kernel(const float* __restrict__ partial, int head_dim, int q_blocks, int k_blocks,
+                                                            float* dq, float* dk) {
+  __shared__ float part[32][33];
+  float* out = blockIdx.y ? dk : dq;
+  if (!out) return;
+  const int first = blockIdx.y ? q_blocks : 0, count = blockIdx.y ? k_blocks : q_blocks;
+  const int e = blockIdx.x * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
+  float v = 0.f;
+  if (e < head_dim)
+    for (int i = share; i < count; i += 32) v += partial[(int64_t)(first + i) * head_dim + e];
+  part[share][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (share == 0 && e < head_dim) {
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v += part[i][threadIdx.x];
+    out[e] = v;
+  }
+}
+
+// Any head_dim up to 512, any even rotary_dim, any alignment: a warp takes one token and keeps one row at a time in shared memory.
+// MODE_GRAD: as heads_grad_kernel.
+template <typename T, int MODE>
+__global__ void __launch_bounds__(HEADS_THREADS) heads_general_kernel(const HeadsArgs a) {
+  extern __shared__ float sm[];
+  const int D = a.head_dim, half = a.rot >> 1;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float* buf = sm + warp * (D + 2 * half);
+  float* cs = buf + D;
+  float* sn = cs + half;
+  int first_seg = 0, last_seg = 1;
+  int64_t blk = blockIdx.x, blocks = gridDim.x;
+  if (MODE == MODE_GRAD) {
+    first_seg = last_seg = (int)blockIdx.x >= a.q_blocks;
+    blk = first_seg ? blockIdx.x - a.q_blocks : blockIdx.x;
+    blocks = first_seg ? gridDim.x - a.q_blocks : a.q_blocks;
+  }
+  const float inv = 1.f / (float)D;
+  float dw[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) dw[j] = 0.f;
+
+  auto rotate = [&](float sign) {
+    for (int i = lane; i < half; i += 32) {
+      const int ia = a.layout == CONQUR_ROPE_HALF ? i : 2 * i, ib = a.layout == CONQUR_ROPE_HALF ? i + half : 2 * i + 1;
+      const float u = buf[ia], v = buf[ib], c = cs[i], s = sign * sn[i];
+      buf[ia] = fmaf(u, c, -v * s);
+      buf[ib] = fmaf(u, s, v * c);
+    }
+    __syncwarp();
+  };
+  auto hadamard = [&]() {
+    for (int m = 1; m < D; m <<= 1) {
+      for (int i = lane; i < D / 2; i += 32) {
+        const int ia = ((i & ~(m - 1)) << 1) | (i & (m - 1));
+        const float u = buf[ia], v = buf[ia | m];
+        buf[ia] = u + v;
+        buf[ia | m] = u - v;
+      }
+      __syncwarp();
+    }
+    for (int i = lane; i < D; i += 32) buf[i] *= a.scale;
+    __syncwarp();
+  };
+  auto warp_sum = [](float v) {
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    return v;
+  };
+
+  for (int64_t token = blk * HEADS_WARPS + warp; token < a.n; token += blocks * HEADS_WARPS) {
+    int64_t b, t;
+    token_of(a, token, b, t);
+    if (half) {
+      const unsigned long long pos = (unsigned long long)a.pos[b * a.pos_b + t];
+      const float amp = (float)__longlong_as_double((long long)a.table[half]);
+      for (int i = lane; i < half; i += 32) angle(pos, a.table[i], amp, cs[i], sn[i]);
+      __syncwarp();
+    }
+    for (int sg = first_seg; sg <= last_seg; ++sg) {
+      const HeadsPtr& g = a.seg[sg];
+      for (int h = MODE == MODE_GRAD ? 0 : blockIdx.y; h < g.heads; h += MODE == MODE_GRAD ? 1 : gridDim.y) {
+        const T* xp = static_cast<const T*>(g.in) + b * g.in_b + t * g.in_t + h * g.in_h;
+        T* op = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + h * g.out_h;
+        float x[16];
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int e = lane + 32 * j;
+          x[j] = e < D ? load1(xp + e) : 0.f;
+          ss = fmaf(x[j], x[j], ss);
+        }
+        if (MODE == MODE_GRAD) {
+          const T* yp = static_cast<const T*>(g.grad) + b * g.grad_b + t * g.grad_t + h * g.grad_h;
+          for (int e = lane; e < D; e += 32) buf[e] = load1(yp + e);
+          __syncwarp();
+          if (a.hadamard) hadamard();
+          rotate(-1.f);
+          float sx = 0.f;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int e = lane + 32 * j;
+            if (e < D) sx = fmaf(load_weight(g.weight, a.weight_bf16, e) * buf[e], x[j], sx);
+          }
+          ss = warp_sum(ss);
+          sx = warp_sum(sx);
+          const float r = 1.f / sqrtf(ss * inv + a.eps);
+          const float k = sx * inv * r * r;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int e = lane + 32 * j;
+            if (e < D) {
+              const float y = buf[e];
+              dw[j] = fmaf(y, x[j] * r, dw[j]);
+              store1(op + e, r * fmaf(load_weight(g.weight, a.weight_bf16, e), y, -x[j] * k));
+            }
+          }
+          __syncwarp();
+          continue;
+        }
+        float r = 1.f;
+        if (MODE == MODE_NORM) r = 1.f / sqrtf(warp_sum(ss) * inv + a.eps);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int e = lane + 32 * j;
+          if (e < D) buf[e] = MODE == MODE_NORM ? x[j] * (r * load_weight(g.weight, a.weight_bf16, e)) : x[j];
+        }
+        __syncwarp();
+        if (a.inverse) {
+          if (a.hadamard) hadamard();
+          rotate(-1.f);
+        } else {
+          rotate(1.f);
+          if (a.hadamard) hadamard();
+        }
+        for (int e = lane; e < D; e += 32) store1(op + e, buf[e]);
+        __syncwarp();
+      }
+    }
+    __syncwarp();
+  }
+  if (MODE == MODE_GRAD) {
+    // the warps' rows, in a fixed order
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int e = lane + 32 * j;
+      if (e < D) buf[e] = dw[j];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < D; e += HEADS_THREADS) {
+      float v = 0.f;
+      for (int k = 0; k < HEADS_WARPS; ++k) v += sm[k * (D + 2 * half) + e];
+      a.partial[(int64_t)blockIdx.x * D + e] = v;
+    }
+  }
+}
+
+struct RopeTable { unsigned long long word[257]; };
+__global__ void rope_table_kernel(const RopeTable t, int words, unsigned long long* out) {
+  for (int i = threadIdx.x; i < words; i += blockDim.x) out[i] = t.word[i];
+}
+
+// ---------------------------------------------------------------------------------------------------- host
+
+bool rope_config_ok(const conqur_rope_config* c) {
+  if (!c || c->struct_size != sizeof(conqur_rope_config) || c->reserved != 0) return false;
+  if (c->rotary_dim < 2 || c->rotary_dim > 512 || (c->rotary_dim & 1)) return false;
+  if (c->scaling < CONQUR_ROPE_SCALE_NONE || c->scaling > CONQUR_ROPE_SCALE_RAMP) return false;
+  if (!(c->theta > 1.0) || !std::isfinite(c->theta)) return false;
+  if (c->scaling != CONQUR_ROPE_SCALE_NONE && (!(c->factor >= 1.0) || !std::isfinite(c->factor))) return false;
+  if (c->scaling == CONQUR_ROPE_SCALE_NTK && c->rotary_dim == 2 && c->factor != 1.0) return false;   // r / (r - 2)
+  if (c->scaling >= CONQUR_ROPE_SCALE_BANDS &&
+      (!(c->low > 0.0) || !(c->high > c->low) || !std::isfinite(c->high) || c->original < 1))
+    return false;
+  return true;
+}
+
+// Frequencies in extended precision: what is held of them, 64 bits of a turn, keeps its last bits at far positions.
+void rope_frequencies(const conqur_rope_config* c, long double* f, double* amp) {
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  const int r = c->rotary_dim;
+  long double log_theta = logl((long double)c->theta);
+  const long double factor = (long double)c->factor;
+  if (c->scaling == CONQUR_ROPE_SCALE_NTK && r > 2) log_theta += logl(factor) * r / (r - 2);
+  long double a = 0, b = 0;
+  *amp = 1.0;
+  if (c->scaling == CONQUR_ROPE_SCALE_RAMP) {
+    auto dim = [&](double turns) { return r * logl((long double)c->original / (two_pi * turns)) / (2 * log_theta); };
+    a = fmaxl(floorl(dim(c->high)), 0);
+    b = fminl(ceill(dim(c->low)), r - 1);
+    *amp = 1.0 + 0.1 * std::log(c->factor);
+  }
+  for (int i = 0; i < r / 2; ++i) {
+    long double v = expl(-log_theta * 2 * i / r);
+    if (c->scaling == CONQUR_ROPE_SCALE_LINEAR) v /= factor;
+    if (c->scaling == CONQUR_ROPE_SCALE_BANDS) {
+      const long double turns = (long double)c->original * v / two_pi;
+      const long double keep = fminl(fmaxl((turns - c->low) / ((long double)c->high - c->low), 0), 1);
+      v *= keep + (1 - keep) / factor;
+    }
+    if (c->scaling == CONQUR_ROPE_SCALE_RAMP) {
+      const long double g = fminl(fmaxl((i - a) / fmaxl(b - a, 0.001L), 0), 1);
+      v = v * (1 - g) + v / factor * g;
+    }
+    f[i] = v;
+  }
+}
+
+int device_sms() {
+  static std::atomic<int> known[64];
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+int launched() { return cudaGetLastError() == cudaSuccess ? CONQUR_OK : CONQUR_ERR_CUDA; }
+
+bool aligned16(const conqur_heads& h, int elem) {
+  return ((reinterpret_cast<uintptr_t>(h.data_dev) | (uintptr_t)(h.batch_stride * elem) | (uintptr_t)(h.token_stride * elem) |
+           (uintptr_t)(h.head_stride * elem)) & 15) == 0;
+}
+
+// Checks and translates a call; `grad`: the backward pass.
+int heads_args(const conqur_heads_call* c, bool norm, bool grad, HeadsArgs& a, bool& vec) {
+  if (!c || c->struct_size != sizeof(conqur_heads_call)) return CONQUR_ERR_INVALID_ARG;
+  if (c->dtype != CONQUR_F32 && c->dtype != CONQUR_BF16) return CONQUR_ERR_INVALID_ARG;
+  if (c->head_dim < 1 || c->head_dim > 512 || c->rotary_dim < 0 || (c->rotary_dim & 1) || c->rotary_dim > c->head_dim) return CONQUR_ERR_INVALID_ARG;
+  if (c->layout != CONQUR_ROPE_HALF && c->layout != CONQUR_ROPE_INTERLEAVED) return CONQUR_ERR_INVALID_ARG;
+  if (c->flags & ~(CONQUR_HEADS_HADAMARD | CONQUR_HEADS_INVERSE)) return CONQUR_ERR_INVALID_ARG;
+  if ((c->flags & CONQUR_HEADS_HADAMARD) && (c->head_dim < 4 || (c->head_dim & (c->head_dim - 1)))) return CONQUR_ERR_INVALID_ARG;
+  if (norm && ((c->flags & CONQUR_HEADS_INVERSE) || !(c->eps > 0.f) || !std::isfinite(c->eps))) return CONQUR_ERR_INVALID_ARG;
+  if (norm && c->weight_dtype != CONQUR_F32 && c->weight_dtype != CONQUR_BF16) return CONQUR_ERR_INVALID_ARG;
+  if (c->q_heads < 1 || c->k_heads < 0 || c->q_heads > 65536 || c->k_heads > 65536) return CONQUR_ERR_INVALID_ARG;
+  if (c->batch < 0 || c->tokens < 0 || (c->tokens > 0 && c->batch > (int64_t)0x7fffffff / c->tokens)) return CONQUR_ERR_INVALID_ARG;
+  const int64_t n = c->batch * c->tokens;
+  if (n > 0) {
+    if (c->rotary_dim > 0 && (!c->positions_dev || !c->table_dev || (reinterpret_cast<uintptr_t>(c->table_dev) & 7) ||
+                              (reinterpret_cast<uintptr_t>(c->positions_dev) & 7)))
+      return CONQUR_ERR_INVALID_ARG;
+  }
+  const int elem = c->dtype == CONQUR_F32 ? 4 : 2;
+  vec = true;
+  for (int i = 0; i < 2; ++i) {
+    const conqur_heads &in = i ? c->k_in : c->q_in, &out = i ? c->k_out : c->q_out, &gr = i ? c->k_grad : c->q_grad;
+    HeadsPtr& p = a.seg[i];
+    p.heads = i ? c->k_heads : c->q_heads;
+    if (p.heads == 0) { p = HeadsPtr{}; continue; }
+    if (n > 0 && (!in.data_dev || !out.data_dev || (grad && !gr.data_dev))) return CONQUR_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(in.data_dev) | reinterpret_cast<uintptr_t>(out.data_dev) | (grad ? reinterpret_cast<uintptr_t>(gr.data_dev) : 0)) & (elem - 1))
+      return CONQUR_ERR_INVALID_ARG;
+    p.in = in.data_dev; p.out = out.data_dev; p.grad = grad ? gr.data_dev : nullptr;
+    p.in_b = in.batch_stride; p.in_t = in.token_stride; p.in_h = in.head_stride;
+    p.out_b = out.batch_stride; p.out_t = out.token_stride; p.out_h = out.head_stride;
+    p.grad_b = gr.batch_stride; p.grad_t = gr.token_stride; p.grad_h = gr.head_stride;
+    p.weight = norm ? (i ? c->k_weight_dev : c->q_weight_dev) : nullptr;
+    if (p.weight && (reinterpret_cast<uintptr_t>(p.weight) & (c->weight_dtype == CONQUR_F32 ? 3 : 1))) return CONQUR_ERR_INVALID_ARG;
+    // every element of an output has a place of its own
+    if ((p.heads > 1 && out.head_stride == 0) || (c->tokens > 1 && out.token_stride == 0) || (c->batch > 1 && out.batch_stride == 0)) return CONQUR_ERR_INVALID_ARG;
+    vec = vec && aligned16(in, elem) && aligned16(out, elem) && (!grad || aligned16(gr, elem));
+  }
+  a.n = n; a.tokens = c->tokens;
+  a.pos = c->positions_dev; a.pos_b = c->positions_batch_stride;
+  a.table = static_cast<const unsigned long long*>(c->table_dev);
+  a.partial = nullptr;
+  a.eps = c->eps; a.scale = (float)(1.0 / sqrt((double)c->head_dim));
+  a.head_dim = c->head_dim; a.rot = c->rotary_dim; a.layout = c->layout;
+  a.hadamard = (c->flags & CONQUR_HEADS_HADAMARD) != 0; a.inverse = (c->flags & CONQUR_HEADS_INVERSE) != 0;
+  a.weight_bf16 = c->weight_dtype == CONQUR_BF16;
+  a.q_blocks = 0;
+  // half-layout pairs have to lie in whole pieces, and with R_3 in pieces that differ in one bit of their number
+  if (c->layout == CONQUR_ROPE_HALF && (c->rotary_dim & 15)) vec = false;
+  if (a.hadamard && c->layout == CONQUR_ROPE_HALF && (c->rotary_dim & (c->rotary_dim - 1))) vec = false;
+  return CONQUR_OK;
+}
+
+// Calls f with the head_dim as a constant where it has an instance; false where not.
+template <typename F>
+bool with_dim(int d, F&& f) {
+  switch (d) {
+    case 64: f(std::integral_constant<int, 64>()); return true;
+    case 80: f(std::integral_constant<int, 80>()); return true;
+    case 96: f(std::integral_constant<int, 96>()); return true;
+    case 112: f(std::integral_constant<int, 112>()); return true;
+    case 128: f(std::integral_constant<int, 128>()); return true;
+    case 192: f(std::integral_constant<int, 192>()); return true;
+    case 256: f(std::integral_constant<int, 256>()); return true;
+    default: return false;
+  }
+}
+
+size_t general_smem(const HeadsArgs& a) { return sizeof(float) * HEADS_WARPS * (a.head_dim + 2 * (a.rot >> 1)); }
+
+template <typename T, bool NORM>
+int forward(const HeadsArgs& a, bool vec, cudaStream_t s) {
+  const int sms = device_sms();
+  if (!sms) return CONQUR_ERR_CUDA;
+  const int64_t blocks = (a.n + HEADS_WARPS - 1) / HEADS_WARPS;
+  // few tokens: their heads go to several warps, up to 24 warps an SM
+  const int64_t want = (24ll * sms + a.n - 1) / a.n;
+  bool done = false;
+  if (vec)
+    done = with_dim(a.head_dim, [&](auto d) {
+      constexpr int D = decltype(d)::value, PW = Row<D>::PER_WARP;
+      const int total = (a.seg[0].heads + PW - 1) / PW + (a.seg[1].heads + PW - 1) / PW;
+      const int split = (int)(want < total ? want : total);
+      heads_kernel<T, D, NORM><<<dim3((unsigned)blocks, split), HEADS_THREADS, 0, s>>>(a);
+    });
+  if (!done) {
+    const int most = a.seg[0].heads > a.seg[1].heads ? a.seg[0].heads : a.seg[1].heads;
+    const int split = (int)(want < most ? want : most);
+    heads_general_kernel<T, NORM ? MODE_NORM : MODE_ROPE><<<dim3((unsigned)blocks, split), HEADS_THREADS, general_smem(a), s>>>(a);
+  }
+  return launched();
+}
+
+template <typename T>
+int backward(HeadsArgs a, bool vec, float* dq, float* dk, cudaStream_t s) {
+  const int sms = device_sms();
+  if (!sms) return CONQUR_ERR_CUDA;
+  int qb = 0, kb = 0;
+  if (a.n > 0) {
+    // as many blocks as stay resident, shared out in proportion to the heads; fewer where there are few tokens
+    const int most = sms * 4 < GRAD_BLOCKS_MAX ? sms * 4 : GRAD_BLOCKS_MAX;
+    const int64_t each = (a.n + HEADS_WARPS - 1) / HEADS_WARPS;
+    const int hq = a.seg[0].heads, hk = a.seg[1].heads;
+    kb = hk ? (int)((int64_t)most * hk / (hq + hk)) : 0;
+    if (hk && kb < 1) kb = 1;
+    qb = most - kb;
+    if (qb < 1) qb = 1;
+    if (qb > each) qb = (int)each;
+    if (kb > each) kb = (int)each;
+    a.q_blocks = qb;
+    bool done = false;
+    if (vec)
+      done = with_dim(a.head_dim, [&](auto d) { heads_grad_kernel<T, decltype(d)::value><<<qb + kb, HEADS_THREADS, 0, s>>>(a); });
+    if (!done) heads_general_kernel<T, MODE_GRAD><<<qb + kb, HEADS_THREADS, general_smem(a), s>>>(a);
+    const int rc = launched();
+    if (rc != CONQUR_OK) return rc;
+  }
+  if (!dq && !dk) return CONQUR_OK;
+  heads_weight_kernel<<<dim3((a.head_dim + 31) / 32, 2), 1024, 0, s>>>(a.partial, a.head_dim, qb, kb, dq, dk);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" int conqur_rope_frequencies(const conqur_rope_config* cfg, double* freq_out, double* amplitude_out) {
+  if (!rope_config_ok(cfg) || !freq_out || !amplitude_out) return CONQUR_ERR_INVALID_ARG;
+  long double f[256];
+  rope_frequencies(cfg, f, amplitude_out);
+  for (int i = 0; i < cfg->rotary_dim / 2; ++i) freq_out[i] = (double)f[i];
+  return CONQUR_OK;
+}
+
+extern "C" size_t conqur_rope_table_bytes(const conqur_rope_config* cfg) {
+  return rope_config_ok(cfg) ? 8 * (size_t)(cfg->rotary_dim / 2 + 1) : 0;
+}
+
+extern "C" int conqur_rope_table(const conqur_rope_config* cfg, void* table_dev, void* cuda_stream) {
+  if (!rope_config_ok(cfg) || !table_dev || (reinterpret_cast<uintptr_t>(table_dev) & 7)) return CONQUR_ERR_INVALID_ARG;
+  long double f[256];
+  double amp;
+  rope_frequencies(cfg, f, &amp);
+  const int half = cfg->rotary_dim / 2;
+  RopeTable t = {};
+  for (int i = 0; i < half; ++i) {
+    // f < 2 pi, so the turn is a fraction; what rounds up to 2^64 is a whole turn
+    const long double turn = f[i] / 6.283185307179586476925286766559005768L;
+    const long double scaled = roundl(ldexpl(turn - floorl(turn), 64));
+    t.word[i] = scaled >= 18446744073709551616.0L ? 0ull : (unsigned long long)scaled;
+  }
+  static_assert(sizeof(double) == sizeof(unsigned long long), "the amplitude's bits take one word");
+  __builtin_memcpy(&t.word[half], &amp, sizeof(double));
+  rope_table_kernel<<<1, 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(t, half + 1, static_cast<unsigned long long*>(table_dev));
+  return launched();
+}
+
+extern "C" int conqur_rope_heads(const conqur_heads_call* call, void* cuda_stream) {
+  HeadsArgs a;
+  bool vec;
+  const int rc = heads_args(call, false, false, a, vec);
+  if (rc != CONQUR_OK || a.n == 0) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return call->dtype == CONQUR_F32 ? forward<float, false>(a, vec, s) : forward<bf16, false>(a, vec, s);
+}
+
+extern "C" int conqur_norm_rope_heads(const conqur_heads_call* call, void* cuda_stream) {
+  HeadsArgs a;
+  bool vec;
+  const int rc = heads_args(call, true, false, a, vec);
+  if (rc != CONQUR_OK || a.n == 0) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return call->dtype == CONQUR_F32 ? forward<float, true>(a, vec, s) : forward<bf16, true>(a, vec, s);
+}
+
+extern "C" size_t conqur_norm_rope_backward_scratch_bytes(int32_t head_dim) {
+  return head_dim < 1 || head_dim > 512 ? 0 : sizeof(float) * GRAD_BLOCKS_MAX * (size_t)head_dim;
+}
+
+extern "C" int conqur_norm_rope_heads_backward(const conqur_heads_call* call, void* scratch_dev, size_t scratch_bytes, void* cuda_stream) {
+  HeadsArgs a;
+  bool vec;
+  const int rc = heads_args(call, true, true, a, vec);
+  if (rc != CONQUR_OK) return rc;
+  if (!scratch_dev || (reinterpret_cast<uintptr_t>(scratch_dev) & 255)) return CONQUR_ERR_INVALID_ARG;
+  if (scratch_bytes < conqur_norm_rope_backward_scratch_bytes(call->head_dim)) return CONQUR_ERR_WORKSPACE_TOO_SMALL;
+  float *dq = call->dq_weight_dev, *dk = call->k_heads ? call->dk_weight_dev : nullptr;
+  if ((reinterpret_cast<uintptr_t>(dq) | reinterpret_cast<uintptr_t>(dk)) & 3) return CONQUR_ERR_INVALID_ARG;
+  a.partial = static_cast<float*>(scratch_dev);
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  return call->dtype == CONQUR_F32 ? backward<float>(a, vec, dq, dk, s) : backward<bf16>(a, vec, dq, dk, s);
+}
