@@ -304,7 +304,7 @@ def _own(s):
         B.conqur_kv_append(s["handle"], s["k"], s["v"], s["slots"])
         return B.conqur_kv_read(s["handle"], s["slots"])
     if "space" not in s:
-        s["space"] = B.attention_workspace(s["handle"], case["b"], case["group"], case["nodes"])
+        s["space"] = B.attention_workspace(s["handle"], case["group"], case["nodes"])
     return B.conqur_tree_attention(s["q"], s["handle"], s["starts"], s["contexts"], s["table"], s["mask"], max_nodes=case["nodes"],
                                    scale=s["scale"], workspace=s["space"])
 
