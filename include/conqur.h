@@ -553,6 +553,95 @@ int conqur_norm_rope_heads(const conqur_heads_call* call, void* cuda_stream);
 size_t conqur_norm_rope_backward_scratch_bytes(int32_t head_dim);
 int conqur_norm_rope_heads_backward(const conqur_heads_call* call, void* scratch_dev, size_t scratch_bytes, void* cuda_stream);
 
+/*
+ * A paged cache of keys and values, the place the rotated keys go to.  Slot s (0 <= s < pages * page_size) is place
+ * s % page_size of page s / page_size.  Per page and key head one contiguous block, page after page, head after head:
+ *   bits 4    key codes page_size x head_dim/2 bytes, value codes the same, key records page_size x 4 bytes, value records the
+ *             same.  Nibble i (0 = lowest) of the 32-bit word w of a token's row holds element 8 w + (0, 2, 4, 6, 1, 3, 5, 7)[i];
+ *             a record is the step as bf16 (low half) and the zero-point code (high half); value = (code - zero-point) step.
+ *             Rows are quantised each by itself (group = head_dim) with the zero-point quantiser of Appendix B:
+ *               lo = c min(y, 0), hi = c max(y, 0), step = bf16((hi - lo) / 15), zero-point = -round(lo / step),
+ *               code = clamp(round(y / step) + zero-point, 0, 15)           round half to even, on the step as it is stored
+ *             The range is widened to hold 0, so that the zero-point is a code (rows with values of both signs have it there
+ *             anyway).  A step below 2^-100 counts as 0: the row is stored as zeros.  A row with a value that is not finite, or
+ *             of 2^127 or more (whose codes' values might not be), is stored as NaN (step NaN).
+ *   bits 16   keys, then values as bf16, each head_dim/64 planes of page_size x 64; the 16-byte piece j of token t's 128-byte row
+ *             lies at piece j ^ (t & 7).
+ * The caller owns the memory; what a page holds before something is written to it does not matter.
+ */
+typedef struct {
+  uint32_t struct_size;     /* = sizeof(conqur_kv_cache) */
+  int32_t  page_size;       /* 16, 32 or 64 tokens */
+  int32_t  kv_heads;        /* 1 .. 65535 */
+  int32_t  head_dim;        /* 64 or 128 */
+  int32_t  bits;            /* 4 or 16 */
+  float    clip_ratio;      /* c in (0, 1], bits 4 (Appendix C uses 1.0 for the cache); 0 = 1 */
+  int64_t  pages;           /* 1 .. 2^31 / page_size */
+  void*    cache_dev;       /* device, 16-byte aligned */
+} conqur_kv_cache;
+
+/* Bytes of the whole cache; 0 on invalid arguments (cache_dev is not looked at). */
+size_t conqur_kv_cache_bytes(const conqur_kv_cache* cache);
+/*
+ * Write n tokens' keys and values into their slots.
+ *   K_dev, V_dev   device bf16: element e of head h of token i at [i token_stride + h head_stride + e]; rows on 16-byte boundaries go 16 bytes at a time
+ *   slots_dev      device int64, one per token; a negative slot: that token is not stored (padding).  A slot beyond the cache is left
+ *                  out and latches CONQUR_ERR_BAD_INDEX.  Where a slot is named twice in one call, it holds parts of either token's rows.
+ * Enqueued on the stream; not synchronised.
+ */
+int conqur_kv_append(const conqur_kv_cache* cache, const void* K_dev, int64_t k_token_stride, int64_t k_head_stride, const void* V_dev,
+                     int64_t v_token_stride, int64_t v_head_stride, int64_t n, const int64_t* slots_dev, void* cuda_stream);
+/*
+ * The values that n slots hold: K_out_dev, V_out_dev device, n x kv_heads x head_dim of out_dtype, dense, 16-byte aligned.  A negative slot gives
+ * zeros, and so does one beyond the cache (latches CONQUR_ERR_BAD_INDEX).  Enqueued on the stream; not synchronised.
+ */
+int conqur_kv_read(const conqur_kv_cache* cache, const int64_t* slots_dev, int64_t n, void* K_out_dev, void* V_out_dev, int32_t out_dtype,
+                   void* cuda_stream);
+/* Synchronises the stream and returns the condition that the cache and attention calls on this device have latched since the last
+ * such call (CONQUR_ERR_BAD_INDEX, CONQUR_ERR_TIMEOUT) or CONQUR_OK; clears it. */
+int conqur_kv_status(void* cuda_stream);
+
+/*
+ * Attention of drafted tokens over the cache.  Sequence b has contexts[b] tokens behind it and T_b = starts[b+1] - starts[b] drafted tokens,
+ * rows starts[b] .. of q; their keys and values lie in the cache at positions contexts[b] + j.  Position l of the sequence is
+ * place l % page_size of page table[b][l / page_size].  Drafted token i sees every position l < contexts[b] and those drafted tokens j
+ * whose bit is set in its mask (a tree: itself and its ancestors); mask_dev NULL: j <= i (a chain; T_b = 1 is ordinary decoding).
+ * Query head h reads key head h / group:
+ *   s_l = scale q . k_l over the positions seen,  out = softmax(s) V,  lse = ln sum exp(s)     (nothing seen: out = 0, lse = -inf)
+ * Arithmetic: products of bf16 values, exact in fp32 (4-bit codes enter as integers), sums, maxima and exponentials in fp32; a probability enters the
+ * product with the values rounded to bf16.  The sums over positions are split over the GPU in a way that depends on
+ * the lengths of all sequences of the call: the same call gives the same bits, another batch around a sequence may change last bits.
+ * A page index outside the cache or a position outside the table is not seen and latches CONQUR_ERR_BAD_INDEX (as do a negative context,
+ * more than max_nodes drafted tokens, and rows outside q).  Values that are not finite reach the rows that see them only.
+ */
+typedef struct {
+  uint32_t struct_size;     /* = sizeof(conqur_tree_call) */
+  int32_t  batch;           /* sequences, 0 .. 65535 */
+  int32_t  group;           /* query heads per key head, 1 .. 64 */
+  int32_t  max_nodes;       /* at least every T_b; 1 .. 64 */
+  float    scale;           /* finite */
+  int32_t  table_width;     /* pages per row of the table */
+  int64_t  rows;            /* rows of q and out; those no sequence names are left as they were */
+  const void* q_dev;        /* device bf16, 16-byte aligned; strides multiples of 8 elements */
+  int64_t  q_token_stride, q_head_stride;
+  void*    out_dev;         /* device bf16, 16-byte aligned; strides multiples of 8 elements; must not overlap q */
+  int64_t  out_token_stride, out_head_stride;
+  float*   lse_dev;         /* device, or NULL: row i, head h at [i lse_token_stride + h] */
+  int64_t  lse_token_stride;
+  const int32_t* starts_dev;      /* batch + 1, not decreasing */
+  const int32_t* contexts_dev;    /* batch */
+  const int32_t* table_dev;
+  int64_t  table_stride;    /* elements from one sequence's row to the next */
+  const uint64_t* mask_dev; /* rows entries, or NULL */
+  void*    workspace_dev;   /* 256-byte aligned; ALL ZERO before its first use, and again after CONQUR_ERR_TIMEOUT; calls leave it as they
+                               need it.  One workspace serves calls that follow one another (one stream, or graphs that do not run together) */
+  size_t   workspace_bytes;
+} conqur_tree_call;
+/* Bytes of a workspace for calls of up to max_nodes * group rows per key head, whatever the batch and the lengths; 0 on invalid arguments. */
+size_t conqur_tree_attention_workspace_bytes(const conqur_kv_cache* cache, int32_t group, int32_t max_nodes);
+/* Enqueued on the stream; not synchronised. */
+int conqur_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* call, void* cuda_stream);
+
 const char* conqur_strerror(int status);
 
 #ifdef __cplusplus

@@ -42,6 +42,8 @@ EXPORTS = [
     "conqur_get_diagnostics", "conqur_fold_scratch_bytes", "conqur_fold_weight", "conqur_hadamard_rows", "conqur_hadamard_status",
     "conqur_rope_frequencies", "conqur_rope_table_bytes", "conqur_rope_table", "conqur_rope_heads", "conqur_norm_rope_heads",
     "conqur_norm_rope_backward_scratch_bytes", "conqur_norm_rope_heads_backward",
+    "conqur_kv_cache_bytes", "conqur_kv_append", "conqur_kv_read", "conqur_kv_status",
+    "conqur_tree_attention_workspace_bytes", "conqur_tree_attention",
     "conqur_strerror",
 ]
 
@@ -89,6 +91,16 @@ class conqur_rope_config(C.Structure):
 
 # conqur_heads_call, packed in one go (its members lie back to back): see include/conqur.h
 _HEADS_CALL = struct.Struct("=IiiiiiifiiqqQqQ" + 4 * "Qqqq" + "QQ" + 2 * "Qqqq" + "QQ")
+
+# conqur_tree_call, the same way
+_TREE_CALL = struct.Struct("=IiiifiqQqqQqqQqQQQqQQQ")
+
+
+class conqur_kv_cache(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("bits", C.c_int32), ("clip_ratio", C.c_float), ("pages", C.c_int64), ("cache_dev", C.c_void_p),
+    ]
 
 
 KERNEL_CLASSES = ["rownorm", "rotate_target", "accumulate", "ns_residual", "ns_poly", "ns_next", "other", "unused"]
@@ -184,6 +196,18 @@ def load() -> C.CDLL:
     lib.conqur_norm_rope_backward_scratch_bytes.argtypes = [i32]
     lib.conqur_norm_rope_heads_backward.restype = C.c_int
     lib.conqur_norm_rope_heads_backward.argtypes = [C.c_char_p, vp, C.c_size_t, vp]
+    lib.conqur_kv_cache_bytes.restype = C.c_size_t
+    lib.conqur_kv_cache_bytes.argtypes = [C.POINTER(conqur_kv_cache)]
+    lib.conqur_kv_append.restype = C.c_int
+    lib.conqur_kv_append.argtypes = [vp, vp, i64, i64, vp, i64, i64, i64, vp, vp]
+    lib.conqur_kv_read.restype = C.c_int
+    lib.conqur_kv_read.argtypes = [vp, vp, i64, vp, vp, i32, vp]
+    lib.conqur_kv_status.restype = C.c_int
+    lib.conqur_kv_status.argtypes = [vp]
+    lib.conqur_tree_attention_workspace_bytes.restype = C.c_size_t
+    lib.conqur_tree_attention_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.conqur_tree_attention.restype = C.c_int
+    lib.conqur_tree_attention.argtypes = [vp, C.c_char_p, vp]
     lib.conqur_strerror.restype = C.c_char_p
     lib.conqur_strerror.argtypes = [C.c_int]
     _lib = lib
@@ -540,6 +564,113 @@ def conqur_norm_rope_heads_backward(q_grad, k_grad, q, k, q_weight, k_weight, po
     if rc != 0:
         raise ConqurError(rc, "conqur_norm_rope_heads_backward")
     return dq, dk, dw[0], None if k is None else dw[1]
+
+
+# ---- the paged key/value cache and the attention of drafted tokens over it ------------------------
+
+class KVCache:
+    """A paged cache on the current device: `pages` pages of `page_size` (16, 32, 64) tokens, codes of 4 bits or bf16 (bits 16).
+
+    data: its memory, a contiguous uint8 tensor (pages, kv_heads, bytes of a block), see include/conqur.h for the layout; made here if None."""
+
+    def __init__(self, pages: int, page_size: int, kv_heads: int, head_dim: int, bits: int = 4, clip_ratio: float = 1.0, data=None):
+        import torch
+        c = conqur_kv_cache(C.sizeof(conqur_kv_cache), page_size, kv_heads, head_dim, bits, clip_ratio, pages, None)
+        nbytes = load().conqur_kv_cache_bytes(C.byref(c))
+        if nbytes == 0:
+            raise ConqurError(-1, "conqur_kv_cache_bytes")
+        if data is None:
+            data = torch.empty((pages, kv_heads, nbytes // (pages * kv_heads)), dtype=torch.uint8, device="cuda")
+        assert data.dtype == torch.uint8 and data.is_contiguous() and data.numel() == nbytes
+        _here(data)
+        c.cache_dev = data.data_ptr()
+        self.data, self.cfg = data, c
+        self.pages, self.page_size, self.kv_heads, self.head_dim, self.bits = pages, page_size, kv_heads, head_dim, bits
+        self._ref = C.addressof(c)
+        self._device = data.get_device()
+
+
+def conqur_kv_append(cache: KVCache, k, v, slots) -> None:
+    """Write keys and values (tokens, kv_heads, head_dim), bf16, into their slots (int64, one per token; negative: not stored)."""
+    stream = _here(cache.data)
+    n = slots.shape[0]
+    shape = (n, cache.kv_heads, cache.head_dim)
+    assert slots.dtype == _torch.int64 and slots.dim() == 1 and slots.get_device() == cache._device and (n <= 1 or slots.stride(0) == 1)
+    for x in (k, v):
+        assert x.dtype == _torch.bfloat16 and x.shape == shape and x.get_device() == cache._device and x.stride(2) == 1
+    rc = (_lib or load()).conqur_kv_append(cache._ref, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
+                                           n, slots.data_ptr(), stream)
+    if rc != 0:
+        raise ConqurError(rc, "conqur_kv_append")
+
+
+def conqur_kv_read(cache: KVCache, slots, dtype=None):
+    """Keys and values (tokens, kv_heads, head_dim) that slots hold, as bf16 (default) or fp32; zeros for a negative slot."""
+    stream = _here(cache.data)
+    n = slots.shape[0]
+    assert slots.dtype == _torch.int64 and slots.dim() == 1 and slots.get_device() == cache._device and (n <= 1 or slots.stride(0) == 1)
+    k, v = _torch.empty((2, n, cache.kv_heads, cache.head_dim), dtype=dtype or _torch.bfloat16, device=cache.data.device)
+    rc = (_lib or load()).conqur_kv_read(cache._ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], stream)
+    if rc != 0:
+        raise ConqurError(rc, "conqur_kv_read")
+    return k, v
+
+
+def conqur_kv_status() -> int:
+    """Synchronise the current stream; condition latched by cache and attention calls since the last such call (0 = ok, -11: an index
+    outside its buffer was left out)."""
+    import torch
+    return int(load().conqur_kv_status(torch.cuda.current_stream().cuda_stream))
+
+
+def attention_workspace(cache: KVCache, group: int, max_nodes: int):
+    """A zeroed workspace for conqur_tree_attention calls of up to max_nodes * group rows a key head that follow one another."""
+    _here(cache.data)
+    nbytes = load().conqur_tree_attention_workspace_bytes(cache._ref, group, max_nodes)
+    if nbytes == 0:
+        raise ConqurError(-1, "conqur_tree_attention_workspace_bytes")
+    return _torch.zeros(nbytes, dtype=_torch.uint8, device=cache.data.device)
+
+
+def conqur_tree_attention(q, cache: KVCache, starts, contexts, table, mask=None, max_nodes: int = 1, scale: Optional[float] = None,
+                          out=None, lse=None, workspace=None):
+    """Attention of drafted tokens over the cache (see include/conqur.h): returns (out, lse).
+
+    q: bf16 (tokens, q_heads, head_dim), the tokens of sequence b in rows starts[b] .. starts[b+1].  starts (b + 1), contexts (b),
+    table (b, pages a sequence): int32.  mask: int64 (tokens,), bit j of a token's: it sees drafted token j of its sequence; None: a
+    chain.  max_nodes: the most tokens a sequence has (at most 64).  scale: 1 / sqrt(head_dim) by default.  out, lse (fp32 (tokens, q_heads)):
+    given or made here; rows that no sequence names stay as they are.  workspace: from attention_workspace; made here if None."""
+    stream = _here(q)
+    t, dev = _torch, cache._device
+    n, heads, d = q.shape
+    batch = contexts.shape[0]
+    group = heads // cache.kv_heads
+    assert q.dtype == t.bfloat16 and q.stride(2) == 1 and q.get_device() == dev and d == cache.head_dim and group * cache.kv_heads == heads
+    i32 = t.int32
+    assert starts.dtype == i32 and starts.shape == (batch + 1,) and starts.is_contiguous() and starts.get_device() == dev
+    assert contexts.dtype == i32 and contexts.dim() == 1 and contexts.is_contiguous() and contexts.get_device() == dev
+    assert table.dtype == i32 and table.dim() == 2 and table.shape[0] == batch and table.get_device() == dev and (table.shape[1] <= 1 or table.stride(1) == 1)
+    mask_ptr = 0
+    if mask is not None:
+        assert mask.dtype == t.int64 and mask.shape == (n,) and mask.is_contiguous() and mask.get_device() == dev
+        mask_ptr = mask.data_ptr()
+    if out is None:
+        out = t.empty((n, heads, d), dtype=t.bfloat16, device=q.device)
+    if lse is None:
+        lse = t.empty((n, heads), dtype=t.float32, device=q.device)
+    assert out.dtype == t.bfloat16 and out.shape == q.shape and out.stride(2) == 1 and out.get_device() == dev
+    assert lse.dtype == t.float32 and lse.shape == (n, heads) and lse.get_device() == dev and (heads == 1 or lse.stride(1) == 1)
+    if workspace is None:
+        workspace = attention_workspace(cache, group, max_nodes)
+    assert workspace.dtype == t.uint8 and workspace.is_contiguous() and workspace.get_device() == dev
+    call = _TREE_CALL.pack(
+        _TREE_CALL.size, batch, group, max_nodes, d ** -0.5 if scale is None else scale, table.shape[1], n,
+        q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(), lse.stride(0),
+        starts.data_ptr(), contexts.data_ptr(), table.data_ptr(), table.stride(0), mask_ptr, workspace.data_ptr(), workspace.numel())
+    rc = (_lib or load()).conqur_tree_attention(cache._ref, call, stream)
+    if rc != 0:
+        raise ConqurError(rc, "conqur_tree_attention")
+    return out, lse
 
 
 # ---- convenience wrapper: owns the workspace tensor, checks status codes ------------------------

@@ -986,7 +986,7 @@ __global__ void __launch_bounds__(256) rownorm_stage_kernel(const TIn* __restric
 }
 
 // fp32 -> bf16 (hi only, lo_elems == 0) or the two-term split [hi; lo].  check: state to arm for a residual product that follows (or null).
-__global__ void split_bf16_kernel(const float* __restrict__ src, __nv_bfloat16* __restrict__ dst, int64_t count,
+static __global__ void split_bf16_kernel(const float* __restrict__ src, __nv_bfloat16* __restrict__ dst, int64_t count,
                                   int64_t lo_elems, DevState* check = nullptr) {
   if (check != nullptr && blockIdx.x == 0 && threadIdx.x == 0) ns_arm_check(check);
   for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4; i < count;
@@ -1012,7 +1012,7 @@ static __global__ void copy_split_kernel(const float* __restrict__ src, float* _
 
 // Second pass of the two-pass step in tensor-core mode (quant modes, or diagnostics): Y (fp32, row-major) ->
 // C' (bf16, row-major) + objective partials (+ diagnostics partials).
-__global__ void __launch_bounds__(256) quant_target_bf16_kernel(const float* __restrict__ Y, int64_t n, int d,
+static __global__ void __launch_bounds__(256) quant_target_bf16_kernel(const float* __restrict__ Y, int64_t n, int d,
                                                                 const float* __restrict__ rnorm,
                                                                 const unsigned int* __restrict__ rowmax_ord,
                                                                 const unsigned int* __restrict__ rowmin_ord,
