@@ -15,8 +15,8 @@
 //   - The work, in tiles of tokens of one sequence, key head and block of rows, is laid end to end and cut into equal runs, one per
 //     resident CTA, whatever the lengths.  A piece of work that is cut leaves its parts (accumulators, maximum, sum) in the workspace; the
 //     last CTA to finish one of its parts adds them up in their order.  No CTA waits for another.
-//   - A producer warp brings pages with bulk copies into a ring of stages; pages are contiguous per head, one copy each.
-// Every wait is bounded; a warp whose wait ran out goes on without reading or writing results, so that the block's barriers match, and the call latches TIMEOUT.
+//   - A warp takes groups of 32 tokens of its own and brings them with asynchronous 16-byte copies into a ring of its own: between the ends of items no
+//     warp waits for another.
 #pragma once
 #include "conqur_tc.cuh"
 
@@ -25,9 +25,9 @@ namespace kv {
 
 struct AttnArgs {
   const uint8_t* cache;
-  long long pages;
-  int page_size, log_page, kv_heads, group, max_nodes, batch, table_width;
-  long long block_bytes, rows;
+  int pages, page_size, log_page, kv_heads, group, max_nodes, batch, table_width;
+  long long block_bytes, page_bytes, rows;   // of a page of one head, of all heads
+  int codes_bytes, plane_bytes;      // of a page's codes of one kind; of a plane
   float scale;                       // times log2 e
   const __nv_bfloat16* q; long long q_t, q_h;
   __nv_bfloat16* out; long long o_t, o_h;
@@ -39,36 +39,31 @@ struct AttnArgs {
   int* flags;
 };
 
-enum { KV_FLAG_BAD_INDEX = 1, KV_FLAG_TIMEOUT = 2 };
+enum { KV_FLAG_BAD_INDEX = 1 };
 
-// BITS of the cache, D, and how a block of 8 NT WM rows and TILE tokens is shared out: WM warps over the rows, WN over the tokens.
-template <int BITS_, int D_, int NT_, int WM_, int WN_, int STAGES_, int MINB_>
+constexpr int ATTN_UNIT = 64;                                    // tokens: what the work is counted and cut in, a multiple of the largest page
+
+constexpr int ATTN_CHUNK = 32;                                   // tokens a warp takes at a time: each half lies in one page
+
+// BITS of the cache, D; a block works on 8 NT query rows with WN warps, each with a ring of STAGES chunks.
+template <int BITS_, int D_, int NT_, int WN_, int STAGES_, int PER_SM_>
 struct AttnCfg {
-  static constexpr int BITS = BITS_, D = D_, NT = NT_, WM = WM_, WN = WN_, STAGES = STAGES_, MINB = MINB_;
-  static constexpr int WARPS = WM * WN, CONSUMERS = 32 * WARPS, THREADS = CONSUMERS + 32;
-  static constexpr int ROWS = 8 * NT * WM;                       // query rows of a block
-  static constexpr int TILE = WN * 16 < 64 ? 64 : WN * 16;       // tokens of a stage: a multiple of the largest page
-  static constexpr int SUBS = TILE / (16 * WN);                  // groups of 16 tokens of a warp
-  static constexpr int TOKEN_BYTES = BITS == 4 ? D + 8 : 4 * D;
-  static constexpr int STAGE_BYTES = TILE * TOKEN_BYTES;
+  static constexpr int BITS = BITS_, D = D_, NT = NT_, WN = WN_, STAGES = STAGES_, PER_SM = PER_SM_;
+  static constexpr int THREADS = 32 * WN;
+  static constexpr int ROWS = 8 * NT;                            // query rows of a block
+  static constexpr int STAGE_BYTES = ATTN_CHUNK * (BITS == 4 ? D + 8 : 4 * D);
   static constexpr int KS = D / 16;                              // k steps of the first product, 16-dimension tiles of the second
-  static constexpr int QFRAG_BYTES = KS * (ROWS / 8) * 32 * 8;
+  static constexpr int QFRAG_BYTES = KS * NT * 32 * 8;
+  static constexpr int HALVES = NT <= 2 ? 2 : 1;                 // groups of 16 tokens that go through the computation together
+  static constexpr bool QREGS = NT <= 2 && PER_SM < 3;           // the rows' fragments stay in registers
   static constexpr int ACC = NT * KS * 4;                        // accumulators a lane
-  static constexpr int PART = ACC + 4 * NT;                      // and its maxima and sums
-  static constexpr int MERGE_BYTES = WN > 1 ? WM * (WN / 2) * PART * 32 * 4 : 0;
-  static constexpr int AUX_BYTES = 512;
-  static constexpr int SMEM = STAGES * STAGE_BYTES + QFRAG_BYTES + MERGE_BYTES + ROWS * 8 + AUX_BYTES;
-  static_assert(SMEM * MINB <= 227 * 1024, "shared memory of an SM");
-  static_assert(TILE % 64 == 0 && SUBS * 16 * WN == TILE, "a stage holds whole pages");
-  static_assert((WN & (WN - 1)) == 0, "the warps' parts are added in halves");
+  static constexpr int PART = ACC + 6 * NT;                      // and its maxima, sums and sums of p z
+  static constexpr int MERGE_BYTES = (WN / 2) * PART * 32 * 4;
+  static constexpr int AUX_BYTES = 1024;
+  static constexpr int SMEM = WN * STAGES * STAGE_BYTES + QFRAG_BYTES + MERGE_BYTES + ROWS * 12 + AUX_BYTES;
+  static_assert((SMEM + 1024) * PER_SM <= 228 * 1024, "shared memory of an SM");
+  static_assert(STAGES <= 16 && (WN & (WN - 1)) == 0, "two bits for every stage; the warps' parts are added in halves");
 };
-
-struct AttnAux {
-  uint64_t full[8], empty[8];
-  uint32_t bad[8];                   // per stage: pages (in order) that could not be read
-  int abort_flag, last;
-};
-static_assert(sizeof(AttnAux) <= 512, "AttnCfg::AUX_BYTES");
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -114,20 +109,28 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   return v;
 }
 __device__ __forceinline__ void named_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
-// codes c in the low nibbles of both halves of w >> shift, less (128 + z) once 128 is added by the exponent: c - z as bf16, exactly
-__device__ __forceinline__ uint32_t codes2(uint32_t w, int shift, uint32_t bias) {
-  const uint32_t v = ((w >> shift) & 0x000F000Fu) | 0x43004300u;
+// Codes enter the products as they lie: a bf16 whose upper byte is 0 is its lower byte times 2^-133, below and above the smallest
+// normal number alike, and the products take such numbers exactly.  So the nibbles at bits 0 and 4 of both halves, masked where they are, are c 2^-133 and
+// 16 c 2^-133; one mask a pair is all the unpacking.  The other operand carries 2^96 (rows) or 2^90 (probabilities), the rows also the 1/16 of their
+// dimensions in odd nibbles, and the sums come back with 2^37 or 2^43.  Zero-points come off the sums: q . (c - z) = q . c - z sum q, and for the values
+// one more tile of the product holds sum p z.
+constexpr float ATTN_Q_UP = 7.922816251426434e28f, ATTN_Q_BACK = 1.37438953472e11f;        // 2^96, 2^(133 - 96)
+constexpr float ATTN_P_UP = 1.2379400392853803e27f, ATTN_P_BACK = 8.796093022208e12f;      // 2^90, 2^(133 - 90)
+__device__ __forceinline__ uint32_t codes_even(uint32_t w) { return w & 0x000F000Fu; }
+__device__ __forceinline__ uint32_t codes_odd(uint32_t w) { return w & 0x00F000F0u; }
+__device__ __forceinline__ float step_of(uint32_t rec) { return __uint_as_float(rec << 16); }
+__device__ __forceinline__ uint32_t zero_of(uint32_t rec) { return (rec >> 16) & 15u; }
+__device__ __forceinline__ float zero_float(uint32_t rec) { return __uint_as_float(zero_of(rec) | 0x4B000000u) - 8388608.f; }
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
   uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(bias));
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ float step_of(uint32_t rec) { return __uint_as_float(rec << 16); }
-__device__ __forceinline__ uint32_t zero_of(uint32_t rec) { return (rec >> 16) & 15u; }       // whatever the bytes are, a code
 
 // The drafted tokens and context of a sequence, and what its work comes to.
 struct Seq {
   int start, nodes, context;
-  int tiles, blocks;                 // tiles of tokens, blocks of rows
+  int tiles, blocks;                 // units of tokens, blocks of rows
 };
 template <typename C>
 __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
@@ -139,12 +142,12 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
   if (s0 < 0 || n < 0 || s1 > a.rows) { n = 0; bad = true; }
   if (n > a.max_nodes) { n = a.max_nodes; bad = true; }
   if (c < 0) { c = 0; bad = true; }
-  if (c > 0x7fffff00) { c = 0x7fffff00; bad = true; }       // positions stay below 2^31
+  if (c > 0x7fff0000) { c = 0x7fff0000; bad = true; }       // positions stay below 2^31
   if (bad && blockIdx.x == 0 && threadIdx.x < 32) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
   s.start = (int)s0;
   s.nodes = (int)n;
   s.context = c;
-  s.tiles = n > 0 ? (int)(((long long)c + n + C::TILE - 1) / C::TILE) : 0;
+  s.tiles = n > 0 ? (int)(((long long)c + n + ATTN_UNIT - 1) / ATTN_UNIT) : 0;
   s.blocks = (int)((n * a.group + C::ROWS - 1) / C::ROWS);
   return s;
 }
@@ -159,7 +162,7 @@ struct Walk {
   int end;                           // the run's last tile of the item, plus one
   long long item_at;                 // place of the item's first tile
 
-  // Every warp works this out for itself: a sum over the sequences, then the one in which the run begins.
+  // One warp: a sum over the sequences, then the one in which the run begins.
   __device__ void begin(const AttnArgs& a) {
     const int lane = threadIdx.x & 31;
     total = 0;
@@ -225,59 +228,118 @@ struct Walk {
   __device__ long long run_begin(int cta) const { return total * cta / ctas; }
 };
 
-// ---------------------------------------------------------------------------------------------- the producer warp
+// ---------------------------------------------------------------------------------------------- copies
 template <typename C>
-__device__ void attn_produce(const AttnArgs& a, uint8_t* stages, AttnAux* aux) {
-  const int lane = threadIdx.x & 31;
-  const int pages_per_tile = C::TILE >> a.log_page;              // at most 8
-  Walk<C> w;
-  w.begin(a);
-  if (w.left <= 0) return;
-  int st = 0;
-  uint32_t phase = 1;                                            // a fresh barrier's previous phase counts as complete
-  bool ok = true, any = false;
-  do {
-    const int head = w.item % a.kv_heads;
-    const long long len = (long long)w.s.context + w.s.nodes;
-    const int* row = a.table + (long long)w.b * a.table_stride;
-    for (int tile = w.tile; ok && tile < w.end; ++tile) {
-      const long long first = ((long long)tile * C::TILE >> a.log_page) + lane;      // this lane's page of the sequence
-      const bool mine = lane < pages_per_tile && (first << a.log_page) < len;
-      long long page = -1;
-      if (mine && first < a.table_width) page = row[first];
-      const bool good = mine && page >= 0 && page < a.pages;
-      const unsigned have = __ballot_sync(0xffffffffu, good), want = __ballot_sync(0xffffffffu, mine);
-      ok = tc_wait_warp(&aux->empty[st], phase, &aux->abort_flag);
-      if (!ok) break;
-      const uint32_t bytes = (uint32_t)a.block_bytes;
-      if (lane == 0) {
-        aux->bad[st] = want & ~have;
-        if (want & ~have) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
-        if (have) ptx::mbar_expect_tx(&aux->full[st], bytes * __popc(have));
-        else ptx::mbar_arrive(&aux->full[st]);
-      }
-      __syncwarp();
-      if (good) {
-        any = true;
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     ::"r"(ptx::smem_u32(stages + (size_t)st * C::STAGE_BYTES + (size_t)lane * bytes)),
-                       "l"(a.cache + (page * a.kv_heads + head) * a.block_bytes), "r"(bytes), "r"(ptx::smem_u32(&aux->full[st]))
-                     : "memory");
-      }
-      if (++st == C::STAGES) { st = 0; phase ^= 1u; }
-    }
-  } while (ok && w.next(a));
-  if (!ok && __any_sync(0xffffffffu, any)) {                     // copies in flight land before the block's shared memory goes
-    const long long t0 = clock64();
-    while (clock64() - t0 < 4000000ll) {}
-  }
+struct AttnAux {
+  Walk<C> ahead[C::WN];              // per warp: the item whose chunks are fetched (the one that is worked on, or a later one)
+  int last, c0, c1;                  // whether this CTA was the last to finish a part of a cut item; the CTAs that have one
+};
+
+// `bytes`: 16, or 0: nothing is read and zeros are stored.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
+
+// A warp's chunks, fetched in the order in which they are worked on, up to STAGES ahead.  A stage holds, of 32 tokens: key codes, value codes, key and
+// value records; or the planes of the keys, then of the values.
+template <typename C>
+struct Fetch {
+  const int* table;                  // the sequence's row
+  const uint8_t* head;               // the key head's block of page 0
+  uint32_t ring;
+  int token, end;                    // the warp's next chunk; end of the item's tokens in this run
+  int page[2];                       // the cache's pages of that chunk's halves, asked for one chunk ahead
+  uint32_t bad;                      // two bits a stage: halves that could not be read
+  int stage;
+  bool more;
+
+  __device__ __forceinline__ void begin(const AttnArgs& a, const Walk<C>& w, uint8_t* smem_ring, Walk<C>* ahead, int wn, int lane) {
+    ring = ptx::smem_u32(smem_ring);
+    bad = 0;
+    stage = 0;
+    more = true;
+    if (lane == 0) *ahead = w;
+    __syncwarp();
+    item(a, w, wn);
+    if (token >= end) settle(a, ahead, wn, lane);
+    ask(a);
+  }
+  __device__ __forceinline__ void item(const AttnArgs& a, const Walk<C>& w, int wn) {
+    table = a.table + (long long)w.b * a.table_stride;
+    head = a.cache + (long long)(w.item % a.kv_heads) * a.block_bytes;
+    token = w.tile * ATTN_UNIT + wn * ATTN_CHUNK;
+    end = min(w.end * ATTN_UNIT, w.s.context + w.s.nodes);
+  }
+  // To the next item that has a chunk for this warp.
+  __device__ __forceinline__ void settle(const AttnArgs& a, Walk<C>* ahead, int wn, int lane) {
+    Walk<C> w = *ahead;
+    while (more && token >= end) {
+      more = w.next(a);
+      if (more) item(a, w, wn);
+    }
+    if (!more) token = end = 0;
+    __syncwarp();
+    if (lane == 0) *ahead = w;
+    __syncwarp();
+  }
+  __device__ __forceinline__ void ask(const AttnArgs& a) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int t = token + 16 * i;
+      page[i] = -1;
+      if (t < end && (t >> a.log_page) < a.table_width) page[i] = table[t >> a.log_page];
+    }
+  }
+  __device__ __forceinline__ void issue(const AttnArgs& a, Walk<C>* ahead, int wn, int lane) {
+    const uint8_t* block[2];
+    int at[2], bytes[2];
+    bad &= ~(3u << (2 * stage));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool good = (unsigned)page[i] < (unsigned)a.pages; // (behind the item's end: -1)
+      bytes[i] = good ? 16 : 0;
+      bad |= (good ? 0u : 1u) << (2 * stage + i);
+      at[i] = (token + 16 * i) & (a.page_size - 1);
+      block[i] = head + (good ? (long long)page[i] * a.page_bytes : 0);
+    }
+    const uint32_t to = ring + stage * C::STAGE_BYTES + lane * 16;
+    if (C::BITS == 4) {
+      constexpr int CODES = 16 * C::D / 2;                     // bytes of 16 tokens: 512 or 1024
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint8_t* p = block[i] + at[i] * (C::D / 2) + lane * 16;
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int j = 0; j < CODES / 512; ++j) copy16(to + (2 * part + i) * CODES + j * 512, p + part * a.codes_bytes + j * 512, bytes[i]);
+      }
+      // records of 16 tokens are 64 bytes: lanes 0-3 and 4-7 the keys' of the two halves, 8-11 and 12-15 the values'
+      const int i = (lane >> 2) & 1;
+      if (lane < 16) copy16(to + 4 * CODES, (i ? block[1] : block[0]) + 2 * a.codes_bytes + ((i ? at[1] : at[0]) + (lane >> 3) * a.page_size) * 4 + (lane & 3) * 16, i ? bytes[1] : bytes[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint8_t* p = block[i] + at[i] * 128 + lane * 16;
+#pragma unroll
+        for (int part = 0; part < C::D / 32; ++part)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) copy16(to + (2 * part + i) * 2048 + j * 512, p + part * a.plane_bytes + j * 512, bytes[i]);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");       // one group a chunk, of zeros at the end of the run
+    stage = stage + 1 == C::STAGES ? 0 : stage + 1;
+    if (more) token += C::WN * ATTN_CHUNK;
+    if (token >= end && more) settle(a, ahead, wn, lane);
+    ask(a);
+  }
+};
 
 // ---------------------------------------------------------------------------------------------- the consumer warps
 template <typename C>
 struct Acc {
   float o[C::NT][C::KS][4];          // O^T: 16-dimension tile x 8 rows; [0], [1] and [2], [3]: dimensions lane / 4 and + 8, rows 2 (lane & 3) and + 1
   float m[C::NT][2], l[C::NT][2];    // bound and sum (this lane's tokens only) of rows 2 (lane & 3) and + 1
+  float z[C::NT][4];                 // sum p z, 4 bits: [0] and [1] of rows 2 (lane & 3) and + 1
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int n = 0; n < C::NT; ++n) {
@@ -287,6 +349,7 @@ struct Acc {
         for (int i = 0; i < 4; ++i) o[n][t][i] = 0.f;
       m[n][0] = m[n][1] = -INFINITY;
       l[n][0] = l[n][1] = 0.f;
+      z[n][0] = z[n][1] = z[n][2] = z[n][3] = 0.f;
     }
   }
   // The factor that takes sums under bound `from` to bound `to` >= from.
@@ -295,6 +358,7 @@ struct Acc {
     const float f = shrink(m[n][j], to);
     m[n][j] = to;
     l[n][j] *= f;
+    z[n][j] *= f;
 #pragma unroll
     for (int t = 0; t < C::KS; ++t) {
       o[n][t][j] *= f;
@@ -309,12 +373,12 @@ struct Acc {
     for (int n = 0; n < C::NT; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float om = get(C::ACC + n * 4 + j), ol = get(C::ACC + n * 4 + 2 + j);
-        // (a bound that is not a number: neither comparison holds, the sums carry it)
+        const float om = get(C::ACC + n * 6 + j), ol = get(C::ACC + n * 6 + 2 + j), oz = C::BITS == 4 ? get(C::ACC + n * 6 + 4 + j) : 0.f;
         const float to = om > m[n][j] ? om : m[n][j];
         rescale(n, j, to);
         const float f = shrink(om, to);
         l[n][j] = fmaf(ol, f, l[n][j]);
+        z[n][j] = fmaf(oz, f, z[n][j]);
 #pragma unroll
         for (int t = 0; t < C::KS; ++t) {
           o[n][t][j] = fmaf(get((n * C::KS + t) * 4 + j), f, o[n][t][j]);
@@ -336,8 +400,9 @@ struct Acc {
         for (int i = 0; i < 4; ++i) put((n * C::KS + t) * 4 + i, o[n][t][i]);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        put(C::ACC + n * 4 + j, m[n][j]);
-        put(C::ACC + n * 4 + 2 + j, l[n][j]);
+        put(C::ACC + n * 6 + j, m[n][j]);
+        put(C::ACC + n * 6 + 2 + j, l[n][j]);
+        if (C::BITS == 4) put(C::ACC + n * 6 + 4 + j, z[n][j]);
       }
     }
   }
@@ -345,25 +410,24 @@ struct Acc {
 
 // The warps' parts of a block of rows into those of wn = 0, by halves (every consumer warp comes here).
 template <typename C>
-__device__ __forceinline__ void attn_merge(Acc<C>& acc, float* buf, int wm, int wn, int lane) {
-  if (C::WN == 1) return;
+__device__ __forceinline__ void attn_merge(Acc<C>& acc, float* buf, int wn, int lane) {
 #pragma unroll 1
   for (int h = C::WN / 2; h >= 1; h >>= 1) {
-    float* p = buf + ((size_t)(wm * (C::WN / 2) + (wn & (h - 1)) ) * C::PART) * 32 + lane;
+    float* p = buf + (size_t)(wn & (h - 1)) * C::PART * 32 + lane;
     if (wn >= h && wn < 2 * h) acc.template store<false>(p, 32);
-    named_sync(C::CONSUMERS);
+    named_sync(C::THREADS);
     if (wn < h) acc.template add<false>(p, 32);
-    named_sync(C::CONSUMERS);
+    named_sync(C::THREADS);
   }
 }
 
-// Query rows of an item in the fragment order of the first product's second operand, and their masks.
+// Query rows of an item in the fragment order of the first product's second operand, their masks and (4 bits) their sums.
 template <typename C>
-__device__ void attn_load_q(const AttnArgs& a, const Seq& s, int item, uint2* frag, unsigned long long* mask) {
+__device__ void attn_load_q(const AttnArgs& a, const Seq& s, int item, uint2* frag, unsigned long long* mask, float* sums) {
   const int head = item % a.kv_heads, first = (item / a.kv_heads) * C::ROWS;
   const int rows = s.nodes * a.group;
-  for (int i = threadIdx.x; i < C::KS * (C::ROWS / 8) * 32; i += C::CONSUMERS) {
-    const int lane = i & 31, n = (i >> 5) % (C::ROWS / 8), ks = (i >> 5) / (C::ROWS / 8);
+  for (int i = threadIdx.x; i < C::KS * C::NT * 32; i += C::THREADS) {
+    const int lane = i & 31, n = (i >> 5) % C::NT, ks = (i >> 5) / C::NT;
     const int r = first + n * 8 + (lane >> 2), c = lane & 3;
     uint2 v = make_uint2(0u, 0u);
     if (r < rows) {
@@ -371,6 +435,8 @@ __device__ void attn_load_q(const AttnArgs& a, const Seq& s, int item, uint2* fr
       const __nv_bfloat16* p = a.q + (long long)(s.start + node) * a.q_t + (long long)(head * a.group + r - node * a.group) * a.q_h;
       if (C::BITS == 4) {
         v = *reinterpret_cast<const uint2*>(p + c * (C::D / 4) + ks * 4);
+        v.x = mul2(v.x, 0x6F806F80u);                         // 2^96: these meet even nibbles
+        v.y = mul2(v.y, 0x6D806D80u);                         // 2^92: these odd ones
       } else {
         v.x = *reinterpret_cast<const uint32_t*>(p + ks * 16 + 2 * c);
         v.y = *reinterpret_cast<const uint32_t*>(p + ks * 16 + 8 + 2 * c);
@@ -378,7 +444,7 @@ __device__ void attn_load_q(const AttnArgs& a, const Seq& s, int item, uint2* fr
     }
     frag[i] = v;
   }
-  for (int i = threadIdx.x; i < C::ROWS; i += C::CONSUMERS) {
+  for (int i = threadIdx.x; i < C::ROWS; i += C::THREADS) {
     const int r = first + i;
     unsigned long long m = 0;
     if (r < rows) {
@@ -388,204 +454,262 @@ __device__ void attn_load_q(const AttnArgs& a, const Seq& s, int item, uint2* fr
     }
     mask[i] = m;
   }
+  if (C::BITS == 4)
+    for (int i = threadIdx.x >> 5; i < C::ROWS; i += C::WN) {
+      const int r = first + i, lane = threadIdx.x & 31;
+      float v = 0.f;
+      if (r < rows) {
+        const int node = r / a.group;
+        const __nv_bfloat16* p = a.q + (long long)(s.start + node) * a.q_t + (long long)(head * a.group + r - node * a.group) * a.q_h + lane * (C::D / 32);
+#pragma unroll
+        for (int e = 0; e < C::D / 32; ++e) v += __bfloat162float(p[e]);
+      }
+#pragma unroll
+      for (int k = 1; k < 32; k <<= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
+      if (lane == 0) sums[i] = v * (1.f / ATTN_Q_BACK);       // in the units of the products
+    }
 }
 
-// 16 tokens of a stage against the warp's rows.  `token`: the first one's place in the stage; `pos`: its position in the sequence.
-// EDGE: some position is not seen by some row (drafted tokens, the end of the sequence, a page that could not be read).
+// A chunk against the rows: HALVES times 16 tokens, from `at` on.  `pos`: the first one's position in the sequence; `bad`: halves that could not be read.
+// EDGE: some position is not seen by some row (drafted tokens, the end of the sequence, a page that could not be read).  Both halves go through
+// each stage of the computation together: what one waits for (products, exponentials) the other fills.
 template <typename C, bool EDGE>
-__device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint32_t stage, int token, long long pos, const Seq& s, uint32_t bad,
-                                            const uint2* frag, const unsigned long long* mask, int lane) {
+__device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint32_t stage, int at, int pos, int context, uint32_t bad,
+                                            const uint2 (&qr)[C::QREGS ? C::KS : 1][C::QREGS ? C::NT : 1], const uint2* frag,
+                                            const unsigned long long* mask, const float* sums, int lane) {
+  constexpr int H = C::HALVES;
   const int g = lane >> 2, c = lane & 3;
-  const int page = token >> a.log_page, at = token & (a.page_size - 1);        // 16 tokens lie in one page
-  const uint32_t block = stage + (uint32_t)page * (uint32_t)a.block_bytes;
-  constexpr int D = C::D, KS = C::KS, NT = C::NT;
-  float sc[NT][4];
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sc[n][i] = 0.f;
+  constexpr int D = C::D, KS = C::KS, NT = C::NT, CT = ATTN_CHUNK;
+  auto query = [&](int k, int n) { return C::QREGS ? qr[C::QREGS ? k : 0][C::QREGS ? n : 0] : frag[(k * NT + n) * 32 + lane]; };
+  float sc[H][NT][4], ks[H][2];
 
   // ---- S^T = K Q^T: rows (tokens) g and g + 8, columns (query rows) 2c and 2c + 1
-  float k0 = a.scale, k1 = a.scale;
-  if (C::BITS == 4) {
-    const uint32_t kr = block + (uint32_t)(a.page_size * D) + (uint32_t)(at + g) * 4;
-    const uint32_t r0 = lds32(kr), r1 = lds32(kr + 32);
-    const uint32_t z0 = 0x43004300u | zero_of(r0) * 0x10001u, z1 = 0x43004300u | zero_of(r1) * 0x10001u;
-    k0 *= step_of(r0);
-    k1 *= step_of(r1);
-    const uint32_t kc = block + (uint32_t)(at + g) * (D / 2) + c * (D / 8);
-    uint32_t w0[D / 32], w1[D / 32];
-    if (D == 128) {
-      const uint4 u = lds128(kc), v = lds128(kc + 8 * (D / 2));
-      w0[0] = u.x; w0[1] = u.y; w0[D / 32 - 2] = u.z; w0[D / 32 - 1] = u.w;
-      w1[0] = v.x; w1[1] = v.y; w1[D / 32 - 2] = v.z; w1[D / 32 - 1] = v.w;
+#pragma unroll
+  for (int u = 0; u < H; ++u) {
+    const int au = at + 16 * u;
+    float sd[NT][4];                   // (the k steps alternate between two sums: a product that waits for the one before it takes several times its issue)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[u][n][i] = sd[n][i] = 0.f;
+    ks[u][0] = ks[u][1] = a.scale;
+    if (C::BITS == 4) {
+      const uint32_t kr = stage + CT * D + au * 4 + g * 4;
+      const uint32_t r0 = lds32(kr), r1 = lds32(kr + 32);
+      const uint32_t kc = stage + au * (D / 2) + lane * (D / 8);         // token g, the c-th quarter of its row
+      uint32_t w0[D / 32], w1[D / 32];
+      if (D == 128) {
+        const uint4 x = lds128(kc), y = lds128(kc + 8 * (D / 2));
+        w0[0] = x.x; w0[1] = x.y; w0[D / 32 - 2] = x.z; w0[D / 32 - 1] = x.w;
+        w1[0] = y.x; w1[1] = y.y; w1[D / 32 - 2] = y.z; w1[D / 32 - 1] = y.w;
+      } else {
+        const uint2 x = lds64(kc), y = lds64(kc + 8 * (D / 2));
+        w0[0] = x.x; w0[1] = x.y;
+        w1[0] = y.x; w1[1] = y.y;
+      }
+      ks[u][0] *= step_of(r0);
+      ks[u][1] *= step_of(r1);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const uint32_t x0 = (k & 1) ? w0[k >> 1] >> 8 : w0[k >> 1], x1 = (k & 1) ? w1[k >> 1] >> 8 : w1[k >> 1];
+        const uint32_t f[4] = {codes_even(x0), codes_even(x1), codes_odd(x0), codes_odd(x1)};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint2 q = query(k, n);
+          mma16816((k & 1) ? sd[n] : sc[u][n], f, q.x, q.y);
+        }
+      }
+      const float z0 = zero_float(r0), z1 = zero_float(r1);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float2 q = *reinterpret_cast<const float2*>(sums + n * 8 + 2 * c);
+        sd[n][0] = fmaf(-z0, q.x, sd[n][0]);
+        sd[n][1] = fmaf(-z0, q.y, sd[n][1]);
+        sd[n][2] = fmaf(-z1, q.x, sd[n][2]);
+        sd[n][3] = fmaf(-z1, q.y, sd[n][3]);
+      }
     } else {
-      const uint2 u = lds64(kc), v = lds64(kc + 8 * (D / 2));
-      w0[0] = u.x; w0[1] = u.y;
-      w1[0] = v.x; w1[1] = v.y;
-    }
+      // lanes 0-7, 8-15, 16-23, 24-31 give the rows of: tokens 0-7 and 8-15 of the first 8 dimensions, then of the second
+      const int t = lane & 15;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const int sh = (k & 1) * 8;
-      const uint32_t f[4] = {codes2(w0[k >> 1], sh, z0), codes2(w1[k >> 1], sh, z1), codes2(w0[k >> 1], sh + 4, z0), codes2(w1[k >> 1], sh + 4, z1)};
+      for (int k = 0; k < KS; ++k) {
+        uint32_t f[4];
+        const int piece = 2 * (k & 3) + (lane >> 4);
+        ldmatrix4(f, stage + (uint32_t)((k >> 2) * CT + au + t) * 128 + ((piece ^ (t & 7)) << 4));
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint2 q = frag[(k * (C::ROWS / 8) + n) * 32 + lane];
-        mma16816(sc[n], f, q.x, q.y);
+        for (int n = 0; n < NT; ++n) {
+          const uint2 q = query(k, n);
+          mma16816((k & 1) ? sd[n] : sc[u][n], f, q.x, q.y);
+        }
       }
     }
-  } else {
-    // lanes 0-7, 8-15, 16-23, 24-31 give the rows of: tokens 0-7 and 8-15 of the first 8 dimensions, then of the second
-    const int t = at + (lane & 15);
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      uint32_t f[4];
-      const int piece = 2 * (k & 3) + (lane >> 4);
-      ldmatrix4(f, block + (uint32_t)((k >> 2) * a.page_size + t) * 128 + ((piece ^ (t & 7)) << 4));
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint2 q = frag[(k * (C::ROWS / 8) + n) * 32 + lane];
-        mma16816(sc[n], f, q.x, q.y);
-      }
-    }
+      for (int i = 0; i < 4; ++i) sc[u][n][i] += sd[n][i];
   }
 
-  // ---- scores, bound, probabilities
-  bool up = false;
+  // ---- exponents against the rows' bounds (none yet: -inf, so that the first scores exceed it)
+  float x[H][NT][4], top = -INFINITY;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+  for (int u = 0; u < H; ++u)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float v = sc[n][i] * ((i & 2) ? k1 : k0);
-      if (EDGE) {
-        const long long p = pos + g + ((i & 2) ? 8 : 0), j = p - s.context;
-        const unsigned long long m = mask[n * 8 + 2 * c + (i & 1)];
-        const bool see = (j < 0 || (j < 64 && ((m >> (j & 63)) & 1ull))) && !((bad >> page) & 1u);
-        if (!see) v = -INFINITY;
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float k = ks[u][i >> 1];
+        if (EDGE) {
+          const int j = pos + 16 * u + g + ((i & 2) ? 8 : 0) - context;
+          const unsigned long long m = mask[n * 8 + 2 * c + (i & 1)];
+          const bool see = (j < 0 || (j < 64 && ((m >> (j & 63)) & 1ull))) && !((bad >> u) & 1u);
+          sc[u][n][i] = see ? sc[u][n][i] * k : -INFINITY;
+          x[u][n][i] = sc[u][n][i] - acc.m[n][i & 1];
+        } else {
+          x[u][n][i] = fmaf(sc[u][n][i], k, -acc.m[n][i & 1]);
+        }
+        top = fmaxf(top, x[u][n][i]);
       }
-      sc[n][i] = v;
-      up = up || v > acc.m[n][i & 1] + 8.f;
-    }
-  }
-  if (__any_sync(0xffffffffu, up)) {
+  if (__any_sync(0xffffffffu, top > 8.f)) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        float t = fmaxf(fmaxf(sc[n][j], sc[n][2 + j]), acc.m[n][j]);
+        float y[H][2], t = acc.m[n][j];
+#pragma unroll
+        for (int u = 0; u < H; ++u) {
+          y[u][0] = EDGE ? sc[u][n][j] : sc[u][n][j] * ks[u][0];
+          y[u][1] = EDGE ? sc[u][n][2 + j] : sc[u][n][2 + j] * ks[u][1];
+          t = fmaxf(t, fmaxf(y[u][0], y[u][1]));
+        }
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, k));
         acc.rescale(n, j, t);
+#pragma unroll
+        for (int u = 0; u < H; ++u) {
+          x[u][n][j] = y[u][0] - t;
+          x[u][n][2 + j] = y[u][1] - t;
+        }
       }
   }
-  float v0 = 1.f, v1 = 1.f;
-  uint32_t rec_v = 0;
-  if (C::BITS == 4) {
-    rec_v = block + (uint32_t)(a.page_size * D) + (uint32_t)(a.page_size + at) * 4;
-    v0 = step_of(lds32(rec_v + g * 4));
-    v1 = step_of(lds32(rec_v + g * 4 + 32));
-  }
-  uint32_t pf[NT][2];
+  // ---- probabilities; with codes, the value's step joins them
+  uint32_t pf[H][NT][2];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    float p[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float m = acc.m[n][i & 1];
-      p[i] = ex2(sc[n][i] - (m == -INFINITY ? 0.f : m));
-      acc.l[n][i & 1] += p[i];
-      if (C::BITS == 4) {
-        p[i] *= (i & 2) ? v1 : v0;                            // the value's step joins its probability
-        if (EDGE && sc[n][i] == -INFINITY) p[i] = 0.f;        // an unseen record may say NaN
-      }
+  for (int u = 0; u < H; ++u) {
+    float v0 = 1.f, v1 = 1.f;
+    if (C::BITS == 4) {
+      const uint32_t vr = stage + CT * (D + 4) + (at + 16 * u) * 4 + g * 4;
+      v0 = step_of(lds32(vr)) * ATTN_P_UP;
+      v1 = step_of(lds32(vr + 32)) * ATTN_P_UP;
     }
-    pf[n][0] = movmatrix(bf16x2(p[0], p[1]));
-    pf[n][1] = movmatrix(bf16x2(p[2], p[3]));
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] = ex2(x[u][n][i]);
+        if (EDGE && sc[u][n][i] == -INFINITY) p[i] = 0.f;          // not seen (and the bound may be -inf still)
+        acc.l[n][i & 1] += p[i];
+        if (C::BITS == 4) {
+          p[i] *= (i & 2) ? v1 : v0;
+          if (EDGE && sc[u][n][i] == -INFINITY) p[i] = 0.f;        // an unseen record may say NaN
+        }
+      }
+      pf[u][n][0] = movmatrix(bf16x2(p[0], p[1]));
+      pf[u][n][1] = movmatrix(bf16x2(p[2], p[3]));
+    }
   }
 
   // ---- O^T += V^T P^T
-  if (C::BITS == 4) {
-    // the pairs of tokens (2c, 2c + 1) and (2c + 8, 2c + 9); dimensions g * D/8 ... of each
-    const uint32_t vr = rec_v + 8 * c;
-    const uint2 ra = lds64(vr), rb = lds64(vr + 32);
-    const uint32_t za = 0x43004300u | zero_of(ra.x) | (zero_of(ra.y) << 16), zb = 0x43004300u | zero_of(rb.x) | (zero_of(rb.y) << 16);
-    const uint32_t vc = block + (uint32_t)(a.page_size * (D / 2)) + (uint32_t)(at + 2 * c) * (D / 2) + g * (D / 16);
-    uint32_t w[4][D / 64];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t p = vc + ((i & 1) + (i >> 1) * 8) * (D / 2);
-      if (D == 128) {
-        const uint2 u = lds64(p);
-        w[i][0] = u.x;
-        w[i][D / 64 - 1] = u.y;
-      } else {
-        w[i][0] = lds32(p);
-      }
-    }
+  for (int u = 0; u < H; ++u) {
+    const int au = at + 16 * u;
+    if (C::BITS == 4) {
+      // the pairs of tokens (2c, 2c + 1) and (2c + 8, 2c + 9); dimensions g * D/8 ... of each
+      const uint32_t vr = stage + CT * (D + 4) + au * 4 + 2 * c * 4;
+      const uint2 ra = lds64(vr), rb = lds64(vr + 32);
+      const uint32_t z[4] = {codes_even(__byte_perm(ra.x, ra.y, 0x7632)), 0u, codes_even(__byte_perm(rb.x, rb.y, 0x7632)), 0u};
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h) {
-      // low halves: elements 0, 2, 4, 6 of the word's eight; high halves: 1, 3, 5, 7
-      const uint32_t al = __byte_perm(w[0][h], w[1][h], 0x5410), ah = __byte_perm(w[0][h], w[1][h], 0x7632);
-      const uint32_t bl = __byte_perm(w[2][h], w[3][h], 0x5410), bh = __byte_perm(w[2][h], w[3][h], 0x7632);
+      for (int n = 0; n < NT; ++n) mma16816(acc.z[n], z, pf[u][n][0], pf[u][n][1]);
+      const uint32_t vc = stage + CT * (D / 2) + au * (D / 2) + 2 * c * (D / 2) + g * (D / 16);
+      uint32_t w[4][D / 64];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t f[4] = {codes2(al, 4 * e, za), codes2(ah, 4 * e, za), codes2(bl, 4 * e, zb), codes2(bh, 4 * e, zb)};
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma16816(acc.o[n][h * 4 + e], f, pf[n][0], pf[n][1]);
-      }
-    }
-  } else {
-    const uint32_t vb = block + (uint32_t)(a.page_size * D * 2);
-    const int t = at + (lane & 7) + ((lane >> 4) << 3);       // lanes 0-7, 8-15: tokens 0-7 of the first and second 8 dimensions; 16-31: tokens 8-15
-    uint32_t odd = 0;                                         // tokens some of whose values are not finite
-    if (EDGE) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t q = lds32(vb + (uint32_t)(at + i) * 128 + lane * 4);
-        const uint32_t q2 = D == 128 ? lds32(vb + (uint32_t)(a.page_size + at + i) * 128 + lane * 4) : 0u;
-        const bool nf = (q & 0x7F80u) == 0x7F80u || (q & 0x7F800000u) == 0x7F800000u || (q2 & 0x7F80u) == 0x7F80u || (q2 & 0x7F800000u) == 0x7F800000u;
-        if (__any_sync(0xffffffffu, nf)) odd |= 1u << i;
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      uint32_t f[4];
-      const int piece = 2 * (k & 3) + ((lane >> 3) & 1);
-      ldmatrix4t(f, vb + (uint32_t)((k >> 2) * a.page_size + t) * 128 + ((piece ^ (t & 7)) << 4));
-      if (EDGE && odd) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if ((f[i] & 0x7F80u) == 0x7F80u) f[i] &= 0xFFFF0000u;
-          if ((f[i] & 0x7F800000u) == 0x7F800000u) f[i] &= 0x0000FFFFu;
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t p = vc + ((i & 1) + (i >> 1) * 8) * (D / 2);
+        if (D == 128) {
+          const uint2 y = lds64(p);
+          w[i][0] = y.x;
+          w[i][D / 64 - 1] = y.y;
+        } else {
+          w[i][0] = lds32(p);
         }
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) mma16816(acc.o[n][k], f, pf[n][0], pf[n][1]);
-    }
-    if (EDGE && odd) {
-      // what was left out above, for the rows that see the token: the product of a probability and a value that is not finite
-#pragma unroll 1
-      for (int i = 0; i < 16; ++i) {
-        if (!((odd >> i) & 1u)) continue;
+      for (int h = 0; h < D / 64; ++h) {
+        // low halves: elements 0, 2, 4, 6 of the word's eight; high halves: 1, 3, 5, 7
+        uint32_t al = __byte_perm(w[0][h], w[1][h], 0x5410), ah = __byte_perm(w[0][h], w[1][h], 0x7632);
+        uint32_t bl = __byte_perm(w[2][h], w[3][h], 0x5410), bh = __byte_perm(w[2][h], w[3][h], 0x7632);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < 4; ++e) {
+          if (e == 2) { al >>= 8; ah >>= 8; bl >>= 8; bh >>= 8; }
+          uint32_t f[4];
+          if (e & 1) { f[0] = codes_odd(al); f[1] = codes_odd(ah); f[2] = codes_odd(bl); f[3] = codes_odd(bh); }
+          else { f[0] = codes_even(al); f[1] = codes_even(ah); f[2] = codes_even(bl); f[3] = codes_even(bh); }
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float mine = (i & 8) ? sc[n][2 + j] : sc[n][j];
-            const float v = __shfl_sync(0xffffffffu, mine, (i & 7) * 4 + c);
-            const float m = acc.m[n][j];
-            if (v == -INFINITY) continue;
-            const float p = ex2(v - (m == -INFINITY ? 0.f : m));
+          for (int n = 0; n < NT; ++n) mma16816(acc.o[n][h * 4 + e], f, pf[u][n][0], pf[u][n][1]);
+        }
+      }
+    } else {
+      const uint32_t vb = stage + CT * D * 2;
+      const int t = (lane & 7) + ((lane >> 4) << 3);       // lanes 0-7, 8-15: tokens 0-7 of the first and second 8 dimensions; 16-31: tokens 8-15
+      uint32_t odd = 0;                                         // tokens some of whose values are not finite
+      if (EDGE) {
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t q = lds32(vb + (uint32_t)(au + i) * 128 + lane * 4);
+          const uint32_t q2 = D == 128 ? lds32(vb + (uint32_t)(CT + au + i) * 128 + lane * 4) : 0u;
+          const bool nf = (q & 0x7F80u) == 0x7F80u || (q & 0x7F800000u) == 0x7F800000u || (q2 & 0x7F80u) == 0x7F80u || (q2 & 0x7F800000u) == 0x7F800000u;
+          if (__any_sync(0xffffffffu, nf)) odd |= 1u << i;
+        }
+      }
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int e = k * 16 + g + 8 * h, tt = at + i;
-                const uint32_t q = lds32(vb + (uint32_t)((e >> 6) * a.page_size + tt) * 128 + (((((e & 63) >> 3) ^ (tt & 7)) << 4) | ((e & 6) << 1)));
-                const float x = (e & 1) ? __uint_as_float(q & 0xFFFF0000u) : __uint_as_float(q << 16);
-                if (!(fabsf(x) <= 3.4028234663852886e38f)) acc.o[n][k][2 * h + j] += p * x;
-              }
+      for (int k = 0; k < KS; ++k) {
+        uint32_t f[4];
+        const int piece = 2 * (k & 3) + ((lane >> 3) & 1);
+        ldmatrix4t(f, vb + (uint32_t)((k >> 2) * CT + au + t) * 128 + ((piece ^ (t & 7)) << 4));
+        if (EDGE && odd) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if ((f[i] & 0x7F80u) == 0x7F80u) f[i] &= 0xFFFF0000u;
+            if ((f[i] & 0x7F800000u) == 0x7F800000u) f[i] &= 0x0000FFFFu;
           }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma16816(acc.o[n][k], f, pf[u][n][0], pf[u][n][1]);
+      }
+      if (EDGE && odd) {
+        // what was left out above, for the rows that see the token: the product of a probability and a value that is not finite
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+          if (!((odd >> i) & 1u)) continue;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float mine = (i & 8) ? sc[u][n][2 + j] : sc[u][n][j];
+              const float v = __shfl_sync(0xffffffffu, mine, (i & 7) * 4 + c);
+              if (v == -INFINITY) continue;
+              const float p = ex2(v - acc.m[n][j]);
+#pragma unroll
+              for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const int e = k * 16 + g + 8 * h, tt = au + i;
+                  const uint32_t q = lds32(vb + (uint32_t)((e >> 6) * CT + tt) * 128 + (((((e & 63) >> 3) ^ (tt & 7)) << 4) | ((e & 6) << 1)));
+                  const float y = (e & 1) ? __uint_as_float(q & 0xFFFF0000u) : __uint_as_float(q << 16);
+                  if (!(fabsf(y) <= 3.4028234663852886e38f)) acc.o[n][k][2 * h + j] += p * y;
+                }
+            }
+        }
       }
     }
   }
@@ -593,9 +717,9 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
 
 // Rows of an item that is complete: normalised, rounded, written.
 template <typename C>
-__device__ void attn_write(const AttnArgs& a, Acc<C>& acc, const Seq& s, int item, int wm, int lane) {
+__device__ void attn_write(const AttnArgs& a, Acc<C>& acc, const Seq& s, int item, int lane) {
   const int g = lane >> 2, c = lane & 3;
-  const int head = item % a.kv_heads, first = (item / a.kv_heads) * C::ROWS + wm * 8 * C::NT;
+  const int head = item % a.kv_heads, first = (item / a.kv_heads) * C::ROWS;
   const int rows = s.nodes * a.group;
 #pragma unroll
   for (int n = 0; n < C::NT; ++n)
@@ -615,7 +739,10 @@ __device__ void attn_write(const AttnArgs& a, Acc<C>& acc, const Seq& s, int ite
         // dimensions g * D/8 + 2t and + 1 of tile t
         uint32_t v[C::KS];
 #pragma unroll
-        for (int t = 0; t < C::KS; ++t) v[t] = bf16x2(acc.o[n][t][j] * inv, acc.o[n][t][2 + j] * inv);
+        for (int t = 0; t < C::KS; ++t) {
+          const float up = (t & 1) ? 0.0625f : 1.f, f = inv * ATTN_P_BACK, z = acc.z[n][j];
+          v[t] = bf16x2(fmaf(acc.o[n][t][j], up, -z) * f, fmaf(acc.o[n][t][2 + j], up, -z) * f);
+        }
         uint4* p = reinterpret_cast<uint4*>(o + g * (C::D / 8));
 #pragma unroll
         for (int t = 0; t < C::KS / 4; ++t) p[t] = make_uint4(v[4 * t], v[4 * t + 1], v[4 * t + 2], v[4 * t + 3]);
@@ -631,94 +758,97 @@ __device__ void attn_write(const AttnArgs& a, Acc<C>& acc, const Seq& s, int ite
 }
 
 template <typename C>
-__global__ void __launch_bounds__(C::THREADS, C::MINB) attn_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(C::THREADS, C::PER_SM) attn_kernel(const AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
-  uint8_t* stages = smem;
-  uint2* frag = reinterpret_cast<uint2*>(smem + C::STAGES * C::STAGE_BYTES);
-  float* merge = reinterpret_cast<float*>(smem + C::STAGES * C::STAGE_BYTES + C::QFRAG_BYTES);
-  unsigned long long* mask = reinterpret_cast<unsigned long long*>(smem + C::STAGES * C::STAGE_BYTES + C::QFRAG_BYTES + C::MERGE_BYTES);
-  AttnAux* aux = reinterpret_cast<AttnAux*>(smem + C::SMEM - C::AUX_BYTES);
-  const int warp = warp_index(), lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < C::STAGES; ++i) {
-      ptx::mbar_init(&aux->full[i], 1);
-      ptx::mbar_init(&aux->empty[i], C::WARPS);
-    }
-    aux->abort_flag = 0;
-    ptx::fence_barrier_init();
-    ptx::fence_proxy_async();
+  constexpr int RINGS = C::WN * C::STAGES * C::STAGE_BYTES;
+  uint2* frag = reinterpret_cast<uint2*>(smem + RINGS);
+  float* merge = reinterpret_cast<float*>(smem + RINGS + C::QFRAG_BYTES);
+  unsigned long long* mask = reinterpret_cast<unsigned long long*>(smem + RINGS + C::QFRAG_BYTES + C::MERGE_BYTES);
+  float* sums = reinterpret_cast<float*>(mask + C::ROWS);
+  AttnAux<C>* aux = reinterpret_cast<AttnAux<C>*>(smem + C::SMEM - C::AUX_BYTES);
+  static_assert(sizeof(AttnAux<C>) <= C::AUX_BYTES, "AttnCfg::AUX_BYTES");
+  const int wn = warp_index(), lane = threadIdx.x & 31;
+  Walk<C> w;
+  if (wn == 0) {
+    w.begin(a);
+    if (lane == 0) aux->ahead[0] = w;
   }
   __syncthreads();
-  if (warp == C::WARPS) {
-    attn_produce<C>(a, stages, aux);
-    return;
-  }
-  const int wm = warp / C::WN, wn = warp % C::WN;
-  Walk<C> w;
-  w.begin(a);
+  w = aux->ahead[0];
   if (w.left <= 0) return;
-  bool dead = false, head_of_run = true;
+  __syncthreads();
+  uint8_t* ring = smem + wn * C::STAGES * C::STAGE_BYTES;
+  Fetch<C> fetch;
+  fetch.begin(a, w, ring, &aux->ahead[wn], wn, lane);
+  for (int i = 0; i < C::STAGES; ++i) fetch.issue(a, &aux->ahead[wn], wn, lane);
+
+  bool head_of_run = true;
   int st = 0;
-  uint32_t phase = 0;
   Acc<C> acc;
   do {
-    attn_load_q<C>(a, w.s, w.item, frag, mask);
+    attn_load_q<C>(a, w.s, w.item, frag, mask, sums);
     acc.clear();
-    named_sync(C::CONSUMERS);
-    const long long len = (long long)w.s.context + w.s.nodes;
-    for (int tile = w.tile; tile < w.end; ++tile) {
-      if (!dead) dead = !tc_wait_warp(&aux->full[st], phase, &aux->abort_flag);
-      if (!dead) {
-        const uint32_t stage = ptx::smem_u32(stages + (size_t)st * C::STAGE_BYTES);
-        const uint32_t bad = *reinterpret_cast<volatile uint32_t*>(&aux->bad[st]);
-        const long long pos0 = (long long)tile * C::TILE;
-#pragma unroll 1
-        for (int sub = 0; sub < C::SUBS; ++sub) {
-          const int token = (sub * C::WN + wn) * 16;
-          const long long pos = pos0 + token;
-          if (pos >= len) break;
-          if (pos + 16 <= w.s.context && bad == 0) attn_tokens<C, false>(a, acc, stage, token, pos, w.s, bad, frag + wm * C::NT * 32, mask + wm * C::NT * 8, lane);
-          else attn_tokens<C, true>(a, acc, stage, token, pos, w.s, bad, frag + wm * C::NT * 32, mask + wm * C::NT * 8, lane);
-        }
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&aux->empty[st]);
-      }
-      if (++st == C::STAGES) { st = 0; phase ^= 1u; }
+    named_sync(C::THREADS);
+    uint2 qr[C::QREGS ? C::KS : 1][C::QREGS ? C::NT : 1];
+    if (C::QREGS) {
+#pragma unroll
+      for (int k = 0; k < C::KS; ++k)
+#pragma unroll
+        for (int n = 0; n < C::NT; ++n) qr[C::QREGS ? k : 0][C::QREGS ? n : 0] = frag[(k * C::NT + n) * 32 + lane];
     }
-    attn_merge<C>(acc, merge, wm, wn, lane);
-    if (*reinterpret_cast<volatile int*>(&aux->abort_flag)) dead = true;      // some warp's tokens are missing
+    const int end = min(w.end * ATTN_UNIT, w.s.context + w.s.nodes);
+    for (int first = w.tile * ATTN_UNIT + wn * ATTN_CHUNK; first < end; first += C::WN * ATTN_CHUNK) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 1) : "memory");
+      __syncwarp();
+      const uint32_t stage = ptx::smem_u32(ring + st * C::STAGE_BYTES);
+      const uint32_t bad = (fetch.bad >> (2 * st)) & 3u;
+      const uint32_t lost = first + 16 < end ? bad : bad & 1u;           // (a second half behind the end is not fetched)
+      if (lost && lane == 0) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
+      const bool edge = first + ATTN_CHUNK > w.s.context || lost;
+#pragma unroll 1
+      for (int at = 0; at < ATTN_CHUNK && first + at < end; at += 16 * C::HALVES) {
+        if (!edge) attn_tokens<C, false>(a, acc, stage, at, 0, 0, 0u, qr, frag, mask, sums, lane);
+        else attn_tokens<C, true>(a, acc, stage, at, first + at, w.s.context, bad >> (at / 16), qr, frag, mask, sums, lane);
+      }
+      __syncwarp();
+      fetch.issue(a, &aux->ahead[wn], wn, lane);               // into the stage that is free now
+      if (++st == C::STAGES) st = 0;
+    }
+    attn_merge<C>(acc, merge, wn, lane);
     const bool whole = w.tile == 0 && w.end == w.s.tiles;
     if (whole) {
-      if (wn == 0 && !dead) attn_write<C>(a, acc, w.s, w.item, wm, lane);
+      if (wn == 0) attn_write<C>(a, acc, w.s, w.item, lane);
     } else {
       // this CTA's part; its first one of the run goes to its first slot
-      constexpr size_t SLOT = (size_t)C::PART * 32 * C::WM;
-      if (wn == 0 && !dead) {
-        acc.template store<true>(a.parts + (2 * (size_t)blockIdx.x + (head_of_run ? 0 : 1)) * SLOT + (size_t)wm * C::PART * 32 + lane, 32);
+      constexpr size_t SLOT = (size_t)C::PART * 32;
+      if (wn == 0) {
+        acc.template store<true>(a.parts + (2 * (size_t)blockIdx.x + (head_of_run ? 0 : 1)) * SLOT + lane, 32);
         __threadfence();
       }
-      const int c0 = w.owner(w.item_at), c1 = w.owner(w.item_at + w.s.tiles - 1);
-      named_sync(C::CONSUMERS);
+      named_sync(C::THREADS);
       if (threadIdx.x == 0) {
+        const int c0 = w.owner(w.item_at), c1 = w.owner(w.item_at + w.s.tiles - 1);
         const unsigned n = (unsigned)(c1 - c0);
-        aux->last = !aux->abort_flag && atomicInc(a.counters + c0, n) == n;
+        aux->last = atomicInc(a.counters + c0, n) == n;
+        aux->c0 = c0;
+        aux->c1 = c1;
         __threadfence();
       }
-      named_sync(C::CONSUMERS);
+      named_sync(C::THREADS);
       if (aux->last) {
+        const int c0 = aux->c0, c1 = aux->c1;
         acc.clear();
         for (int k = c0 + wn; k <= c1; k += C::WN) {
           // the part of CTA k: its run begins with it unless the item began inside the run
-          acc.template add<true>(a.parts + (2 * (size_t)k + (w.run_begin(k) < w.item_at ? 1 : 0)) * SLOT + (size_t)wm * C::PART * 32 + lane, 32);
+          acc.template add<true>(a.parts + (2 * (size_t)k + (w.run_begin(k) < w.item_at ? 1 : 0)) * SLOT + lane, 32);
         }
-        attn_merge<C>(acc, merge, wm, wn, lane);
-        if (wn == 0 && !dead) attn_write<C>(a, acc, w.s, w.item, wm, lane);
+        attn_merge<C>(acc, merge, wn, lane);
+        if (wn == 0) attn_write<C>(a, acc, w.s, w.item, lane);
       }
     }
     head_of_run = false;
-    named_sync(C::CONSUMERS);                                  // the fragments may be replaced
+    named_sync(C::THREADS);                                  // the fragments may be replaced
   } while (w.next(a));
-  if (dead && lane == 0) atomicOr(a.flags, KV_FLAG_TIMEOUT);
 }
 
 }  // namespace kv

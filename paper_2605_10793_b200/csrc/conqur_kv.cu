@@ -275,29 +275,29 @@ int rows_args(const conqur_kv_cache* c, int64_t n, const int64_t* slots, RowsArg
 
 struct AttnVariant {
   void (*kernel)(const kv::AttnArgs);
-  int rows, tile, threads, smem, slot_floats;
+  int rows, threads, smem, slot_floats;
 };
 template <typename C>
 AttnVariant variant() {
-  return {kv::attn_kernel<C>, C::ROWS, C::TILE, C::THREADS, C::SMEM, C::PART * 32 * C::WM};
+  return {kv::attn_kernel<C>, C::ROWS, C::THREADS, C::SMEM, C::PART * 32};
 }
-constexpr int ATTN_VARIANTS = 5;
+constexpr int ATTN_VARIANTS = 3;
 constexpr int ATTN_CTAS_MAX = 592;        // runs of work: 4 per SM
 constexpr size_t ATTN_COUNTER_BYTES = (ATTN_CTAS_MAX * sizeof(unsigned) + 255) / 256 * 256;      // at the workspace's start in every call
 
 template <int BITS, int D>
 AttnVariant by_rows(int i) {
-  constexpr bool small = BITS == 4;        // stages of codes are a quarter of those of bf16: two blocks an SM
+  // chunks of codes are a quarter of those of bf16: two blocks an SM
+  constexpr bool small = BITS == 4;
+  constexpr int halves = 128 / D;
   switch (i) {
-    case 0: return variant<kv::AttnCfg<BITS, D, 1, 1, 8, small ? 4 : (D == 64 ? 5 : 3), small ? 2 : 1>>();
-    case 1: return variant<kv::AttnCfg<BITS, D, 2, 1, 8, small ? 4 : (D == 64 ? 4 : 2), 1>>();
-    case 2: return variant<kv::AttnCfg<BITS, D, 4, 1, 8, small ? 4 : 2, 1>>();
-    case 3: return variant<kv::AttnCfg<BITS, D, 4, 2, 4, BITS == 16 && D == 128 ? 3 : 4, 1>>();
-    default: return variant<kv::AttnCfg<BITS, D, 4, 4, 2, BITS == 16 && D == 128 ? 3 : 4, 1>>();
+    case 0: return variant<kv::AttnCfg<BITS, D, 1, small ? 8 : 4, (small ? 2 : 3) * halves, small ? 2 : 1>>();
+    case 1: return variant<kv::AttnCfg<BITS, D, 2, small ? 8 : 4, (small ? 4 : 2) * halves, 1>>();
+    default: return variant<kv::AttnCfg<BITS, D, 4, small ? 8 : 4, (small ? 3 : 2) * halves, 1>>();
   }
 }
-// The fewest rows that hold a sequence's, or blocks of 128.
-int rows_class(int rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 3 : 4; }
+// The fewest rows that hold a sequence's, or blocks of 32.
+int rows_class(int rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : 2; }
 AttnVariant pick(int bits, int d, int cls) {
   if (bits == 4) return d == 64 ? by_rows<4, 64>(cls) : by_rows<4, 128>(cls);
   return d == 64 ? by_rows<16, 64>(cls) : by_rows<16, 128>(cls);
@@ -385,7 +385,7 @@ extern "C" int conqur_kv_status(void* cuda_stream) {
   int f = 0;
   if (!flags || cudaMemcpyAsync(&f, flags, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) return CONQUR_ERR_CUDA;
   if (f && (cudaMemsetAsync(flags, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)) return CONQUR_ERR_CUDA;
-  return (f & kv::KV_FLAG_TIMEOUT) ? CONQUR_ERR_TIMEOUT : (f & kv::KV_FLAG_BAD_INDEX) ? CONQUR_ERR_BAD_INDEX : CONQUR_OK;
+  return (f & kv::KV_FLAG_BAD_INDEX) ? CONQUR_ERR_BAD_INDEX : CONQUR_OK;
 }
 
 extern "C" size_t conqur_tree_attention_workspace_bytes(const conqur_kv_cache* cache, int32_t group, int32_t max_nodes) {
@@ -418,10 +418,12 @@ extern "C" int conqur_tree_attention(const conqur_kv_cache* cache, const conqur_
   const AttnVariant v = pick(cache->bits, cache->head_dim, cls);
   kv::AttnArgs a = {};
   a.cache = static_cast<const uint8_t*>(cache->cache_dev);
-  a.pages = cache->pages; a.page_size = cache->page_size; a.log_page = log2_of(cache->page_size); a.kv_heads = cache->kv_heads;
+  a.pages = (int)cache->pages; a.page_size = cache->page_size; a.log_page = log2_of(cache->page_size); a.kv_heads = cache->kv_heads;
   a.group = c->group; a.max_nodes = c->max_nodes; a.batch = c->batch; a.table_width = c->table_width;
-  a.block_bytes = block_bytes(cache); a.rows = c->rows;
-  a.scale = (float)((double)c->scale * 1.4426950408889634);
+  a.block_bytes = block_bytes(cache); a.page_bytes = a.block_bytes * cache->kv_heads;
+  a.codes_bytes = cache->page_size * cache->head_dim / 2; a.plane_bytes = cache->page_size * 128;
+  a.rows = c->rows;
+  a.scale = (float)((double)c->scale * 1.4426950408889634) * (cache->bits == 4 ? kv::ATTN_Q_BACK : 1.f);
   a.q = static_cast<const bf16*>(c->q_dev); a.q_t = c->q_token_stride; a.q_h = c->q_head_stride;
   a.out = static_cast<bf16*>(c->out_dev); a.o_t = c->out_token_stride; a.o_h = c->out_head_stride;
   a.lse = c->lse_dev; a.lse_t = c->lse_token_stride;

@@ -4,7 +4,9 @@ The cache's codes are exact: the step is rounded to bf16 before it divides, ties
 
 Attention's bounds, per element of a row with probabilities p_l and largest sum of |q k| scale over the positions S: a score is a sum of d
 exact products in fp32, 16 at a time, which leaves at most 2^-18 S with its scaling (delta); exponentials and sums add 2^-20; a probability is rounded to bf16
-before it meets the values (2^-8): |error| <= (2^-8 + 2 delta + 2^-19) sum p |v| + 2^-8 |out|.  lse: delta, 2^-20 of its size and the rounding of a sum of up to
+before it meets the values (2^-8): |error| <= (2^-8 + 2 delta + 2^-19) sum p |v| + 2^-8 |out|.  With 4 bits the products hold codes, not
+code - zero-point: sums of up to 15 sum p step, rounded (or cut, 2^-23) once per 16 tokens of one of eight warps and in some 12 additions of parts, less sum p
+zero-point step: (positions / 128 + 12) 2^-23 15 sum p step more.  lse: delta, 2^-20 of its size and the rounding of a sum of up to
 2^11 terms a lane, 2^-13."""
 import numpy as np
 import pytest
@@ -166,6 +168,12 @@ def _tree_masks(rng, nodes, kind):
     return out
 
 
+def _codes_bound(step, k, q, seen, scale):
+    """What the sums of codes may add (see above); step (positions,), zeros where the cache holds bf16."""
+    w = K.attend(q, k, step[:, None], seen, scale)[0]
+    return (len(step) / 128 + 12) * 2.0 ** -23 * 15 * w
+
+
 class Setup:
     """A batch of sequences whose keys and values lie in scattered pages; q packed with spare rows behind."""
 
@@ -185,7 +193,7 @@ class Setup:
             at += n
         self.data = torch.full((pages, hk, K.block_bytes(page, d, bits)), 0xFF, dtype=torch.uint8, device="cuda")   # reads as NaN where nothing was written
         self.cache = B.KVCache(pages, page, hk, d, bits=bits, data=self.data)
-        self.k, self.v = [], []
+        self.k, self.v, self.step = [], [], []
         for b, n in enumerate(lengths):
             k, v = K.bf16(r.standard_normal((n, hk, d))), K.bf16(r.standard_normal((n, hk, d)))
             k[..., : d // 16] = K.bf16(k[..., : d // 16] * 3)
@@ -194,6 +202,7 @@ class Setup:
                 B.conqur_kv_append(self.cache, _dev(k), _dev(v), torch.from_numpy(slots).cuda())
             self.k.append(K.values(k, bits) if n else k)
             self.v.append(K.values(v, bits) if n else v)
+            self.step.append(K.quantise(v)[2][..., 0] if n and bits == 4 else np.zeros((n, hk)))
         self.masks = _tree_masks(r, nodes, kind)
         self.starts = np.concatenate([[0], np.cumsum(nodes)]).astype(np.int32)
         rows = int(self.starts[-1]) + 2
@@ -228,7 +237,7 @@ class Setup:
                 kh = h // self.group
                 want, wl, mass, size = K.attend(self.q[a:a + n, h], self.k[b][:, kh], self.v[b][:, kh], seen, scale)
                 delta = 2.0 ** -18 * size
-                bound = (2.0 ** -8 + 2 * delta[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want) + 1e-30
+                bound = (2.0 ** -8 + 2 * delta[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want) + 1e-30 + _codes_bound(self.step[b][:, kh], self.k[b][:, kh], self.q[a:a + n, h], seen, scale)
                 err = np.abs(o[a:a + n, h] - want)
                 assert (err <= bound).all(), (b, h, float((err / bound).max()))
                 none = np.isneginf(wl)
@@ -359,6 +368,7 @@ def test_bad_pages_contexts_and_starts_are_left_out_and_told_of():
                 seen[:, 16:32] = False
                 want, _, mass, size = K.attend(s.q[2:5, h], s.k[1][:, kh], s.v[1][:, kh], seen, 64 ** -0.5)
                 bound = (2.0 ** -8 + 2.0 ** -17 * size[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want)
+                bound += _codes_bound(s.step[1][:, kh], s.k[1][:, kh], s.q[2:5, h], seen, 64 ** -0.5)
                 assert (np.abs(out[2:5, h].float().cpu().numpy() - want) <= bound).all()
             s.dev["table"].copy_(old)
         # a table too narrow for a context, a negative context, more tokens than max_nodes, rows outside q
@@ -432,12 +442,13 @@ def test_strided_queries_no_lse_streams_and_graphs():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         out = step()
-    ks, vs = [], []
+    ks, vs, sv = [], [], []
     for a, b, c in steps:
         q.copy_(a)
         k.copy_(b)
         v.copy_(c)
         graph.replay()
+        sv.append(K.quantise(c.float().cpu().numpy().astype(np.float64))[2][..., 0])
         ks.append(K.values(b.float().cpu().numpy().astype(np.float64), 4))
         vs.append(K.values(c.float().cpu().numpy().astype(np.float64), 4))
         if len(ks) in (1, 16, 17, 33, 40):
@@ -447,6 +458,7 @@ def test_strided_queries_no_lse_streams_and_graphs():
                     qq = a[i, h].float().cpu().numpy()[None]
                     want, _, mass, size = K.attend(qq, kk, vv, np.ones((1, len(ks)), bool), 128 ** -0.5)
                     bound = (2.0 ** -8 + 2.0 ** -17 * size[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want)
+                    bound += _codes_bound(np.array([x[i, h // 4] for x in sv]), kk, qq, np.ones((1, len(ks)), bool), 128 ** -0.5)
                     assert (np.abs(out[i, h].float().cpu().numpy() - want) <= bound).all()
     assert B.conqur_kv_status() == 0 and warm.shape == out.shape
 
@@ -511,5 +523,6 @@ def test_rotated_heads_through_the_cache_to_attention():
     for h in range(hq):
         want, _, mass, size = K.attend(qs[:, h], kv[0][:, h // 4], kv[1][:, h // 4], seen, d ** -0.5)
         bound = (2.0 ** -8 + 2.0 ** -17 * size[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want)
+        bound += _codes_bound(K.quantise(x[:, hq + hk:])[2][:, h // 4, 0], kv[0][:, h // 4], qs[:, h], seen, d ** -0.5)
         assert (np.abs(out[:, h].float().cpu().numpy() - want) <= bound).all()
     assert B.conqur_kv_status() == 0
