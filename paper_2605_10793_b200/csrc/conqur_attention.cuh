@@ -15,8 +15,8 @@
 //   - The work, in tiles of tokens of one sequence, key head and block of rows, is laid end to end and cut into equal runs, one per
 //     resident CTA, whatever the lengths.  A piece of work that is cut leaves its parts (accumulators, maximum, sum) in the workspace; the
 //     last CTA to finish one of its parts adds them up in their order.  No CTA waits for another.
-//   - A warp takes groups of 32 tokens of its own and brings them with asynchronous 16-byte copies into a ring of its own: between the ends of items no
-//     warp waits for another.
+//   - A warp takes groups of 32 tokens of its own and brings them with asynchronous 16-byte copies into a ring of its own: no warp waits for another
+//     but the one that adds up an item's parts: the warps take turns at that, the others go on with the next item.
 #pragma once
 #include "conqur_tc.cuh"
 
@@ -53,14 +53,13 @@ struct AttnCfg {
   static constexpr int ROWS = 8 * NT;                            // query rows of a block
   static constexpr int STAGE_BYTES = ATTN_CHUNK * (BITS == 4 ? D + 8 : 4 * D);
   static constexpr int KS = D / 16;                              // k steps of the first product, 16-dimension tiles of the second
-  static constexpr int QFRAG_BYTES = KS * NT * 32 * 8;
   static constexpr int HALVES = NT <= 2 ? 2 : 1;                 // groups of 16 tokens that go through the computation together
   static constexpr bool QREGS = NT <= 2 && PER_SM < 3;           // the rows' fragments stay in registers
   static constexpr int ACC = NT * KS * 4;                        // accumulators a lane
   static constexpr int PART = ACC + 6 * NT;                      // and its maxima, sums and sums of p z
-  static constexpr int MERGE_BYTES = (WN / 2) * PART * 32 * 4;
+  static constexpr int MERGE_BYTES = (WN - 1) * PART * 32 * 4;
   static constexpr int AUX_BYTES = 1024;
-  static constexpr int SMEM = WN * STAGES * STAGE_BYTES + QFRAG_BYTES + MERGE_BYTES + ROWS * 12 + AUX_BYTES;
+  static constexpr int SMEM = WN * STAGES * STAGE_BYTES + MERGE_BYTES + AUX_BYTES;
   static_assert((SMEM + 1024) * PER_SM <= 228 * 1024, "shared memory of an SM");
   static_assert(STAGES <= 16 && (WN & (WN - 1)) == 0, "two bits for every stage; the warps' parts are added in halves");
 };
@@ -108,7 +107,9 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ void named_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_sync(int bar, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int bar, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(bar), "r"(threads) : "memory"); }
+enum { BAR_ALL = 1, BAR_STORED = 2, BAR_ADDED = 3 };      // BAR_ADDED and the one behind it, in turn
 // Codes enter the products as they lie: a bf16 whose upper byte is 0 is its lower byte times 2^-133, below and above the smallest
 // normal number alike, and the products take such numbers exactly.  So the nibbles at bits 0 and 4 of both halves, masked where they are, are c 2^-133 and
 // 16 c 2^-133; one mask a pair is all the unpacking.  The other operand carries 2^96 (rows) or 2^90 (probabilities), the rows also the 1/16 of their
@@ -232,7 +233,9 @@ struct Walk {
 template <typename C>
 struct AttnAux {
   Walk<C> ahead[C::WN];              // per warp: the item whose chunks are fetched (the one that is worked on, or a later one)
-  int last, c0, c1;                  // whether this CTA was the last to finish a part of a cut item; the CTAs that have one
+  // cut items of which this CTA finished the last part (at most the first and the last of its run): added up when the run is done
+  struct { Seq s; int item, c0, c1; long long item_at; } todo[2];
+  int todos;
 };
 
 // `bytes`: 16, or 0: nothing is read and zeros are stored.
@@ -408,79 +411,96 @@ struct Acc {
   }
 };
 
-// The warps' parts of a block of rows into those of wn = 0, by halves (every consumer warp comes here).
+// The warps' parts of a block of rows into those of wn = 0, by halves (every warp comes here).
 template <typename C>
 __device__ __forceinline__ void attn_merge(Acc<C>& acc, float* buf, int wn, int lane) {
 #pragma unroll 1
   for (int h = C::WN / 2; h >= 1; h >>= 1) {
     float* p = buf + (size_t)(wn & (h - 1)) * C::PART * 32 + lane;
     if (wn >= h && wn < 2 * h) acc.template store<false>(p, 32);
-    named_sync(C::THREADS);
+    bar_sync(BAR_ALL, C::THREADS);
     if (wn < h) acc.template add<false>(p, 32);
-    named_sync(C::THREADS);
+    bar_sync(BAR_ALL, C::THREADS);
   }
 }
 
-// Query rows of an item in the fragment order of the first product's second operand, their masks and (4 bits) their sums.
+// The query rows of an item as a lane meets them in the first product's second operand: row g = lane / 4 of each eight, a quarter of its dimensions.
 template <typename C>
-__device__ void attn_load_q(const AttnArgs& a, const Seq& s, int item, uint2* frag, unsigned long long* mask, float* sums) {
-  const int head = item % a.kv_heads, first = (item / a.kv_heads) * C::ROWS;
-  const int rows = s.nodes * a.group;
-  for (int i = threadIdx.x; i < C::KS * C::NT * 32; i += C::THREADS) {
-    const int lane = i & 31, n = (i >> 5) % C::NT, ks = (i >> 5) / C::NT;
-    const int r = first + n * 8 + (lane >> 2), c = lane & 3;
+struct Query {
+  const __nv_bfloat16* p[C::NT];     // NULL: no such row
+  uint2 f[C::QREGS ? C::KS : 1][C::QREGS ? C::NT : 1];
+  float sum[C::NT][2];               // 4 bits: sums of rows 2 (lane & 3) and + 1, in the units of the products
+  int first, rows;                   // the block's first row; rows of the sequence
+
+  __device__ __forceinline__ uint2 load(int k, int n, int c) const {
     uint2 v = make_uint2(0u, 0u);
-    if (r < rows) {
-      const int node = r / a.group;
-      const __nv_bfloat16* p = a.q + (long long)(s.start + node) * a.q_t + (long long)(head * a.group + r - node * a.group) * a.q_h;
+    if (p[n]) {
       if (C::BITS == 4) {
-        v = *reinterpret_cast<const uint2*>(p + c * (C::D / 4) + ks * 4);
-        v.x = mul2(v.x, 0x6F806F80u);                         // 2^96: these meet even nibbles
-        v.y = mul2(v.y, 0x6D806D80u);                         // 2^92: these odd ones
+        v = *reinterpret_cast<const uint2*>(p[n] + c * (C::D / 4) + k * 4);
       } else {
-        v.x = *reinterpret_cast<const uint32_t*>(p + ks * 16 + 2 * c);
-        v.y = *reinterpret_cast<const uint32_t*>(p + ks * 16 + 8 + 2 * c);
+        v.x = *reinterpret_cast<const uint32_t*>(p[n] + k * 16 + 2 * c);
+        v.y = *reinterpret_cast<const uint32_t*>(p[n] + k * 16 + 8 + 2 * c);
       }
     }
-    frag[i] = v;
+    return v;
   }
-  for (int i = threadIdx.x; i < C::ROWS; i += C::THREADS) {
-    const int r = first + i;
-    unsigned long long m = 0;
-    if (r < rows) {
-      const int node = r / a.group;
-      m = a.mask ? a.mask[s.start + node] : (2ull << node) - 1ull;
-      if (s.nodes < 64) m &= (1ull << s.nodes) - 1ull;
-    }
-    mask[i] = m;
+  static __device__ __forceinline__ uint2 scaled(uint2 v) {
+    // even nibbles meet the first two of four dimensions with 2^96, odd ones the others with 2^92
+    return C::BITS == 4 ? make_uint2(mul2(v.x, 0x6F806F80u), mul2(v.y, 0x6D806D80u)) : v;
   }
-  if (C::BITS == 4)
-    for (int i = threadIdx.x >> 5; i < C::ROWS; i += C::WN) {
-      const int r = first + i, lane = threadIdx.x & 31;
-      float v = 0.f;
-      if (r < rows) {
-        const int node = r / a.group;
-        const __nv_bfloat16* p = a.q + (long long)(s.start + node) * a.q_t + (long long)(head * a.group + r - node * a.group) * a.q_h + lane * (C::D / 32);
+  __device__ __forceinline__ uint2 get(int k, int n, int c) const {
+    return C::QREGS ? f[C::QREGS ? k : 0][C::QREGS ? n : 0] : scaled(load(k, n, c));
+  }
+  __device__ __forceinline__ void begin(const AttnArgs& a, const Seq& s, int item, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+    const int head = item % a.kv_heads;
+    first = (item / a.kv_heads) * C::ROWS;
+    rows = s.nodes * a.group;
 #pragma unroll
-        for (int e = 0; e < C::D / 32; ++e) v += __bfloat162float(p[e]);
+    for (int n = 0; n < C::NT; ++n) {
+      const int r = first + n * 8 + g, node = r / a.group;
+      p[n] = r < rows ? a.q + (long long)(s.start + node) * a.q_t + (long long)(head * a.group + r - node * a.group) * a.q_h : nullptr;
+    }
+#pragma unroll
+    for (int n = 0; n < C::NT; ++n) {
+      float part = 0.f;
+#pragma unroll
+      for (int k = 0; k < C::KS; ++k) {
+        const uint2 v = load(k, n, c);
+        if (C::BITS == 4) {
+          const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x)), y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
+          part += (x.x + x.y) + (y.x + y.y);
+        }
+        if (C::QREGS) f[C::QREGS ? k : 0][C::QREGS ? n : 0] = scaled(v);
       }
-#pragma unroll
-      for (int k = 1; k < 32; k <<= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
-      if (lane == 0) sums[i] = v * (1.f / ATTN_Q_BACK);       // in the units of the products
+      if (C::BITS == 4) {
+        part += __shfl_xor_sync(0xffffffffu, part, 1);
+        part += __shfl_xor_sync(0xffffffffu, part, 2);
+        sum[n][0] = __shfl_sync(0xffffffffu, part, 8 * c) * (1.f / ATTN_Q_BACK);
+        sum[n][1] = __shfl_sync(0xffffffffu, part, 8 * c + 4) * (1.f / ATTN_Q_BACK);
+      }
     }
-}
+  }
+  // The drafted tokens that row n * 8 + 2 (lane & 3) + j sees.
+  __device__ __forceinline__ unsigned long long mask(const AttnArgs& a, const Seq& s, int n, int j, int c) const {
+    const int r = first + n * 8 + 2 * c + j;
+    if (r >= rows) return 0ull;
+    const int node = r / a.group;
+    unsigned long long m = a.mask ? a.mask[s.start + node] : (2ull << node) - 1ull;
+    if (s.nodes < 64) m &= (1ull << s.nodes) - 1ull;
+    return m;
+  }
+};
 
 // A chunk against the rows: HALVES times 16 tokens, from `at` on.  `pos`: the first one's position in the sequence; `bad`: halves that could not be read.
 // EDGE: some position is not seen by some row (drafted tokens, the end of the sequence, a page that could not be read).  Both halves go through
 // each stage of the computation together: what one waits for (products, exponentials) the other fills.
 template <typename C, bool EDGE>
-__device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint32_t stage, int at, int pos, int context, uint32_t bad,
-                                            const uint2 (&qr)[C::QREGS ? C::KS : 1][C::QREGS ? C::NT : 1], const uint2* frag,
-                                            const unsigned long long* mask, const float* sums, int lane) {
+__device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint32_t stage, int at, int pos, const Seq& s, uint32_t bad,
+                                            const Query<C>& query, int lane) {
   constexpr int H = C::HALVES;
   const int g = lane >> 2, c = lane & 3;
   constexpr int D = C::D, KS = C::KS, NT = C::NT, CT = ATTN_CHUNK;
-  auto query = [&](int k, int n) { return C::QREGS ? qr[C::QREGS ? k : 0][C::QREGS ? n : 0] : frag[(k * NT + n) * 32 + lane]; };
   float sc[H][NT][4], ks[H][2];
 
   // ---- S^T = K Q^T: rows (tokens) g and g + 8, columns (query rows) 2c and 2c + 1
@@ -515,18 +535,17 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
         const uint32_t f[4] = {codes_even(x0), codes_even(x1), codes_odd(x0), codes_odd(x1)};
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint2 q = query(k, n);
+          const uint2 q = query.get(k, n, c);
           mma16816((k & 1) ? sd[n] : sc[u][n], f, q.x, q.y);
         }
       }
       const float z0 = zero_float(r0), z1 = zero_float(r1);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const float2 q = *reinterpret_cast<const float2*>(sums + n * 8 + 2 * c);
-        sd[n][0] = fmaf(-z0, q.x, sd[n][0]);
-        sd[n][1] = fmaf(-z0, q.y, sd[n][1]);
-        sd[n][2] = fmaf(-z1, q.x, sd[n][2]);
-        sd[n][3] = fmaf(-z1, q.y, sd[n][3]);
+        sd[n][0] = fmaf(-z0, query.sum[n][0], sd[n][0]);
+        sd[n][1] = fmaf(-z0, query.sum[n][1], sd[n][1]);
+        sd[n][2] = fmaf(-z1, query.sum[n][0], sd[n][2]);
+        sd[n][3] = fmaf(-z1, query.sum[n][1], sd[n][3]);
       }
     } else {
       // lanes 0-7, 8-15, 16-23, 24-31 give the rows of: tokens 0-7 and 8-15 of the first 8 dimensions, then of the second
@@ -538,7 +557,7 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
         ldmatrix4(f, stage + (uint32_t)((k >> 2) * CT + au + t) * 128 + ((piece ^ (t & 7)) << 4));
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint2 q = query(k, n);
+          const uint2 q = query.get(k, n, c);
           mma16816((k & 1) ? sd[n] : sc[u][n], f, q.x, q.y);
         }
       }
@@ -551,6 +570,13 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
 
   // ---- exponents against the rows' bounds (none yet: -inf, so that the first scores exceed it)
   float x[H][NT][4], top = -INFINITY;
+  unsigned long long mask[NT][2];
+  if (EDGE)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      mask[n][0] = query.mask(a, s, n, 0, c);
+      mask[n][1] = query.mask(a, s, n, 1, c);
+    }
 #pragma unroll
   for (int u = 0; u < H; ++u)
 #pragma unroll
@@ -559,8 +585,8 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
       for (int i = 0; i < 4; ++i) {
         const float k = ks[u][i >> 1];
         if (EDGE) {
-          const int j = pos + 16 * u + g + ((i & 2) ? 8 : 0) - context;
-          const unsigned long long m = mask[n * 8 + 2 * c + (i & 1)];
+          const int j = pos + 16 * u + g + ((i & 2) ? 8 : 0) - s.context;
+          const unsigned long long m = mask[n][i & 1];
           const bool see = (j < 0 || (j < 64 && ((m >> (j & 63)) & 1ull))) && !((bad >> u) & 1u);
           sc[u][n][i] = see ? sc[u][n][i] * k : -INFINITY;
           x[u][n][i] = sc[u][n][i] - acc.m[n][i & 1];
@@ -761,17 +787,18 @@ template <typename C>
 __global__ void __launch_bounds__(C::THREADS, C::PER_SM) attn_kernel(const AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   constexpr int RINGS = C::WN * C::STAGES * C::STAGE_BYTES;
-  uint2* frag = reinterpret_cast<uint2*>(smem + RINGS);
-  float* merge = reinterpret_cast<float*>(smem + RINGS + C::QFRAG_BYTES);
-  unsigned long long* mask = reinterpret_cast<unsigned long long*>(smem + RINGS + C::QFRAG_BYTES + C::MERGE_BYTES);
-  float* sums = reinterpret_cast<float*>(mask + C::ROWS);
-  AttnAux<C>* aux = reinterpret_cast<AttnAux<C>*>(smem + C::SMEM - C::AUX_BYTES);
+  constexpr size_t SLOT = (size_t)C::PART * 32;
+  float* merge = reinterpret_cast<float*>(smem + RINGS);
+  AttnAux<C>* aux = reinterpret_cast<AttnAux<C>*>(smem + RINGS + C::MERGE_BYTES);
   static_assert(sizeof(AttnAux<C>) <= C::AUX_BYTES, "AttnCfg::AUX_BYTES");
   const int wn = warp_index(), lane = threadIdx.x & 31;
   Walk<C> w;
   if (wn == 0) {
     w.begin(a);
-    if (lane == 0) aux->ahead[0] = w;
+    if (lane == 0) {
+      aux->ahead[0] = w;
+      aux->todos = 0;
+    }
   }
   __syncthreads();
   w = aux->ahead[0];
@@ -783,19 +810,13 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) attn_kernel(const AttnA
   for (int i = 0; i < C::STAGES; ++i) fetch.issue(a, &aux->ahead[wn], wn, lane);
 
   bool head_of_run = true;
-  int st = 0;
+  int st = 0, adder = 0, turn = 0;                             // the warp that adds up the present item's parts; items so far, modulo 2
   Acc<C> acc;
+  bool more;
   do {
-    attn_load_q<C>(a, w.s, w.item, frag, mask, sums);
+    Query<C> query;
+    query.begin(a, w.s, w.item, lane);
     acc.clear();
-    named_sync(C::THREADS);
-    uint2 qr[C::QREGS ? C::KS : 1][C::QREGS ? C::NT : 1];
-    if (C::QREGS) {
-#pragma unroll
-      for (int k = 0; k < C::KS; ++k)
-#pragma unroll
-        for (int n = 0; n < C::NT; ++n) qr[C::QREGS ? k : 0][C::QREGS ? n : 0] = frag[(k * C::NT + n) * 32 + lane];
-    }
     const int end = min(w.end * ATTN_UNIT, w.s.context + w.s.nodes);
     for (int first = w.tile * ATTN_UNIT + wn * ATTN_CHUNK; first < end; first += C::WN * ATTN_CHUNK) {
       asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 1) : "memory");
@@ -807,48 +828,63 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) attn_kernel(const AttnA
       const bool edge = first + ATTN_CHUNK > w.s.context || lost;
 #pragma unroll 1
       for (int at = 0; at < ATTN_CHUNK && first + at < end; at += 16 * C::HALVES) {
-        if (!edge) attn_tokens<C, false>(a, acc, stage, at, 0, 0, 0u, qr, frag, mask, sums, lane);
-        else attn_tokens<C, true>(a, acc, stage, at, first + at, w.s.context, bad >> (at / 16), qr, frag, mask, sums, lane);
+        if (!edge) attn_tokens<C, false>(a, acc, stage, at, 0, w.s, 0u, query, lane);
+        else attn_tokens<C, true>(a, acc, stage, at, first + at, w.s, bad >> (at / 16), query, lane);
       }
       __syncwarp();
       fetch.issue(a, &aux->ahead[wn], wn, lane);               // into the stage that is free now
-      if (++st == C::STAGES) st = 0;
+      st = st + 1 == C::STAGES ? 0 : st + 1;
     }
-    attn_merge<C>(acc, merge, wn, lane);
-    const bool whole = w.tile == 0 && w.end == w.s.tiles;
-    if (whole) {
-      if (wn == 0) attn_write<C>(a, acc, w.s, w.item, lane);
+    // Parts are stored once those of the item before are added up; its adder knows that, and may be an item ahead of the warps that still ask: hence
+    // two barriers in turn.
+    if (!head_of_run && wn != (adder + C::WN - 1) % C::WN) bar_sync(BAR_ADDED + (turn ^ 1), C::THREADS);
+    if (wn != adder) {
+      acc.template store<false>(merge + (size_t)(wn < adder ? wn : wn - 1) * SLOT + lane, 32);
+      bar_arrive(BAR_STORED, C::THREADS);
     } else {
-      // this CTA's part; its first one of the run goes to its first slot
-      constexpr size_t SLOT = (size_t)C::PART * 32;
-      if (wn == 0) {
+      bar_sync(BAR_STORED, C::THREADS);
+#pragma unroll 1
+      for (int k = 0; k < C::WN - 1; ++k) acc.template add<false>(merge + (size_t)k * SLOT + lane, 32);
+      if (w.tile == 0 && w.end == w.s.tiles) {
+        attn_write<C>(a, acc, w.s, w.item, lane);
+      } else {
+        // this CTA's part; its first one of the run goes to its first slot
         acc.template store<true>(a.parts + (2 * (size_t)blockIdx.x + (head_of_run ? 0 : 1)) * SLOT + lane, 32);
         __threadfence();
-      }
-      named_sync(C::THREADS);
-      if (threadIdx.x == 0) {
-        const int c0 = w.owner(w.item_at), c1 = w.owner(w.item_at + w.s.tiles - 1);
-        const unsigned n = (unsigned)(c1 - c0);
-        aux->last = atomicInc(a.counters + c0, n) == n;
-        aux->c0 = c0;
-        aux->c1 = c1;
-        __threadfence();
-      }
-      named_sync(C::THREADS);
-      if (aux->last) {
-        const int c0 = aux->c0, c1 = aux->c1;
-        acc.clear();
-        for (int k = c0 + wn; k <= c1; k += C::WN) {
-          // the part of CTA k: its run begins with it unless the item began inside the run
-          acc.template add<true>(a.parts + (2 * (size_t)k + (w.run_begin(k) < w.item_at ? 1 : 0)) * SLOT + lane, 32);
+        __syncwarp();
+        if (lane == 0) {
+          const int c0 = w.owner(w.item_at), c1 = w.owner(w.item_at + w.s.tiles - 1);
+          const unsigned n = (unsigned)(c1 - c0);
+          if (atomicInc(a.counters + c0, n) == n) {
+            auto& d = aux->todo[aux->todos++];
+            d.s = w.s;
+            d.item = w.item;
+            d.c0 = c0;
+            d.c1 = c1;
+            d.item_at = w.item_at;
+          }
+          __threadfence();
         }
-        attn_merge<C>(acc, merge, wn, lane);
-        if (wn == 0) attn_write<C>(a, acc, w.s, w.item, lane);
+        __syncwarp();
       }
+      bar_arrive(BAR_ADDED + turn, C::THREADS);
     }
     head_of_run = false;
-    named_sync(C::THREADS);                                  // the fragments may be replaced
-  } while (w.next(a));
+    more = w.next(a);
+    adder = adder + 1 == C::WN ? 0 : adder + 1;
+    turn ^= 1;
+  } while (more);
+  if (wn != (adder + C::WN - 1) % C::WN) bar_sync(BAR_ADDED + (turn ^ 1), C::THREADS);
+  bar_sync(BAR_ALL, C::THREADS);
+  for (int i = 0; i < aux->todos; ++i) {
+    const auto& d = aux->todo[i];
+    acc.clear();
+    for (int k = d.c0 + wn; k <= d.c1; k += C::WN)
+      // the part of CTA k: its run begins with it unless the item began inside the run
+      acc.template add<true>(a.parts + (2 * (size_t)k + (w.run_begin(k) < d.item_at ? 1 : 0)) * SLOT + lane, 32);
+    attn_merge<C>(acc, merge, wn, lane);
+    if (wn == 0) attn_write<C>(a, acc, d.s, d.item, lane);
+  }
 }
 
 }  // namespace kv

@@ -293,7 +293,7 @@ AttnVariant by_rows(int i) {
   switch (i) {
     case 0: return variant<kv::AttnCfg<BITS, D, 1, small ? 8 : 4, (small ? 2 : 3) * halves, small ? 2 : 1>>();
     case 1: return variant<kv::AttnCfg<BITS, D, 2, small ? 8 : 4, (small ? 4 : 2) * halves, 1>>();
-    default: return variant<kv::AttnCfg<BITS, D, 4, small ? 8 : 4, (small ? 3 : 2) * halves, 1>>();
+    default: return variant<kv::AttnCfg<BITS, D, 4, small ? 8 : 4, 2 * halves, 1>>();
   }
 }
 // The fewest rows that hold a sequence's, or blocks of 32.
