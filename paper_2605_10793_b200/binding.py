@@ -91,6 +91,7 @@ class conqur_rope_config(C.Structure):
 
 # conqur_heads_call, packed in one go (its members lie back to back): see include/conqur.h
 _HEADS_CALL = struct.Struct("=IiiiiiifiiqqQqQ" + 4 * "Qqqq" + "QQ" + 2 * "Qqqq" + "QQ")
+_HEADS_CALL_SIZE = _HEADS_CALL.size
 
 # conqur_tree_call, the same way
 _TREE_CALL = struct.Struct("=IiiifiqQqqQqqQqQQQqQQQ")
@@ -411,21 +412,19 @@ def conqur_hadamard_status() -> int:
 # ---- query and key heads: position rotation, per-head norms, R_3 ---------------------------------
 
 _torch = None
+_DTYPES: dict = {}                                # torch dtype -> C code (torch is imported on first use)
 
 
 def _here(x) -> int:
     """Handle of the current stream; the tensor has to live on the current device."""
-    global _torch, _DTYPES
+    global _torch
     if _torch is None:
         import torch
         _torch = torch
-        _DTYPES = {torch.float32: CONQUR_F32, torch.bfloat16: CONQUR_BF16}
-    dev = _torch.cuda.current_device()
-    assert x.is_cuda and x.get_device() == dev, "tensors have to live on the current CUDA device"
+        _DTYPES.update({torch.float32: CONQUR_F32, torch.bfloat16: CONQUR_BF16})
+    dev = x.get_device()                          # -1: not a CUDA tensor
+    assert dev >= 0 and dev == _torch.cuda.current_device(), "tensors have to live on the current CUDA device"
     return _torch._C._cuda_getCurrentRawStream(dev)
-
-
-_DTYPES: dict = {}                                # torch dtype -> C code (torch is imported on first use)
 
 
 def rope_config(rotary_dim: int, theta=10000.0, scaling="none", factor=1.0, low=0.0, high=0.0, original=0) -> conqur_rope_config:
@@ -459,7 +458,7 @@ class Rope:
         rc = load().conqur_rope_table(C.byref(self.cfg), self.table.data_ptr(), _here(self.table))
         if rc != 0:
             raise ConqurError(rc, "conqur_rope_table")
-        self._ptr = self.table.data_ptr()
+        self._ptr, self.device = self.table.data_ptr(), self.table.get_device()
 
     def frequencies(self) -> Tuple[np.ndarray, float]:
         return conqur_rope_frequencies(self.cfg)
@@ -468,51 +467,62 @@ class Rope:
 _NO_HEADS = (0, 0, 0, 0)
 
 
-def _heads(x, like=None):
+def _heads(x):
     """(data, batch stride, token stride, head stride) of a (tokens, heads, d) or (batch, tokens, heads, d) tensor."""
-    assert like is None or (x.dtype == like.dtype and x.shape == like.shape and x.is_cuda and x.get_device() == like.get_device())
     st = x.stride()
     assert st[-1] == 1 or x.shape[-1] == 1, "the elements of a head have to lie back to back"
     return (x.data_ptr(), 0, st[0], st[1]) if len(st) == 3 else (x.data_ptr(), st[0], st[1], st[2])
 
 
-def _heads_call(q, k, positions, rope, flags, eps, q_weight, k_weight, q_out, k_out, q_grad=None, k_grad=None, dq_weight=0, dk_weight=0):
-    shape = q.shape
-    assert len(shape) in (3, 4) and q.dtype in _DTYPES
-    batch, tokens = (1, shape[0]) if len(shape) == 3 else (shape[0], shape[1])
-    d, device = shape[-1], q.get_device()
-    k_heads = 0
+def _heads_call(q, k, positions, rope, flags, eps, q_weight, k_weight, out, q_grad=None, k_grad=None, dq_weight=0, dk_weight=0):
+    """The packed conqur_heads_call and the outputs (those given, or new ones)."""
+    shape, dtype, device = q.shape, q.dtype, q.get_device()
+    code = _DTYPES[dtype]
+    four = len(shape) == 4
+    assert four or len(shape) == 3
+    batch, tokens = (shape[0], shape[1]) if four else (1, shape[0])
+    d = shape[-1]
+    if out is None:
+        q_out = _torch.empty_like(q, memory_format=_torch.contiguous_format)
+        k_out = None if k is None else _torch.empty_like(k, memory_format=_torch.contiguous_format)
+    else:
+        q_out, k_out = out
+        assert q_out.shape == shape and q_out.dtype == dtype and q_out.get_device() == device
+        assert k is None or (k_out.shape == k.shape and k_out.dtype == dtype and k_out.get_device() == device)
+    k_heads, ki, ko = 0, _NO_HEADS, _NO_HEADS
     if k is not None:
-        assert k.dtype == q.dtype and k.get_device() == device and k.dim() == q.dim() and k.shape[:-2] == shape[:-2] and k.shape[-1] == d
-        k_heads = k.shape[-2]
+        ks = k.shape
+        assert k.dtype == dtype and k.get_device() == device and ks[:-2] == shape[:-2] and ks[-1] == d
+        k_heads, ki, ko = ks[-2], _heads(k), _heads(k_out)
     pos = pos_b = table = rotary = layout = 0
     if rope is not None:
-        assert positions.dtype == _torch.int64 and positions.get_device() == device and rope.table.get_device() == device
-        if positions.dim() == 1:
-            assert positions.shape[0] == tokens and (positions.stride(0) == 1 or tokens <= 1)
+        ps, st = positions.shape, positions.stride()
+        assert positions.dtype is _torch.int64 and positions.get_device() == device == rope.device and (st[-1] == 1 or tokens <= 1)
+        if len(ps) == 1:
+            assert ps[0] == tokens
         else:
-            assert positions.shape == (batch, tokens) and (positions.stride(1) == 1 or tokens <= 1)
-            pos_b = positions.stride(0)
+            assert ps == (batch, tokens)
+            pos_b = st[0]
         pos, table, rotary, layout = positions.data_ptr(), rope._ptr, rope.rotary_dim, rope.layout
     wq = wk = wt = 0
     for w in (q_weight, k_weight):
         if w is not None:
-            assert w.get_device() == device and w.shape == (d,) and w.is_contiguous() and w.dtype in _DTYPES
+            assert w.get_device() == device and w.shape == (d,) and w.is_contiguous()
+            wt = _DTYPES[w.dtype]
     if q_weight is not None:
-        wq, wt = q_weight.data_ptr(), _DTYPES[q_weight.dtype]
+        assert k_weight is None or k_weight.dtype == q_weight.dtype
+        wq = q_weight.data_ptr()
     if k_weight is not None:
-        assert q_weight is None or k_weight.dtype == q_weight.dtype
-        wk, wt = k_weight.data_ptr(), _DTYPES[k_weight.dtype]
-    return _HEADS_CALL.pack(
-        _HEADS_CALL.size, _DTYPES[q.dtype], d, rotary, layout, flags, wt, eps, shape[-2], k_heads, batch, tokens, pos, pos_b, table,
-        *_heads(q), *(_NO_HEADS if k is None else _heads(k)), *_heads(q_out, q), *(_NO_HEADS if k is None else _heads(k_out, k)), wq, wk,
-        *(_NO_HEADS if q_grad is None else _heads(q_grad, q)), *(_NO_HEADS if k_grad is None else _heads(k_grad, k)), dq_weight, dk_weight)
-
-
-def _outputs(q, k, out):
-    if out is None:
-        return _torch.empty(q.shape, dtype=q.dtype, device=q.device), None if k is None else _torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    return out
+        wk = k_weight.data_ptr()
+    qg = kg = _NO_HEADS
+    if q_grad is not None:
+        assert q_grad.shape == shape and q_grad.dtype == dtype and q_grad.get_device() == device
+        qg = _heads(q_grad)
+    if k_grad is not None:
+        assert k_grad.shape == k.shape and k_grad.dtype == dtype and k_grad.get_device() == device
+        kg = _heads(k_grad)
+    return _HEADS_CALL.pack(_HEADS_CALL_SIZE, code, d, rotary, layout, flags, wt, eps, shape[-2], k_heads, batch, tokens, pos, pos_b, table,
+                            *_heads(q), *ki, *_heads(q_out), *ko, wq, wk, *qg, *kg, dq_weight, dk_weight), q_out, k_out
 
 
 def conqur_rope_heads(q, k, positions, rope: Optional[Rope], hadamard=False, inverse=False, out=None):
@@ -522,9 +532,9 @@ def conqur_rope_heads(q, k, positions, rope: Optional[Rope], hadamard=False, inv
     q, k: fp32 / bf16 CUDA tensors (tokens, heads, d) or (batch, tokens, heads, d), any strides but the last; k may be None.
     positions: int64 (tokens,) or (batch, tokens).  out: (q_out, k_out), which may be (q, k).  Returns (q_out, k_out)."""
     stream = _here(q)
-    q_out, k_out = _outputs(q, k, out)
     flags = (CONQUR_HEADS_HADAMARD if hadamard else 0) | (CONQUR_HEADS_INVERSE if inverse else 0)
-    rc = (_lib or load()).conqur_rope_heads(_heads_call(q, k, positions, rope, flags, 0.0, None, None, q_out, k_out), stream)
+    call, q_out, k_out = _heads_call(q, k, positions, rope, flags, 0.0, None, None, out)
+    rc = (_lib or load()).conqur_rope_heads(call, stream)
     if rc != 0:
         raise ConqurError(rc, "conqur_rope_heads")
     return q_out, k_out
@@ -533,8 +543,7 @@ def conqur_rope_heads(q, k, positions, rope: Optional[Rope], hadamard=False, inv
 def conqur_norm_rope_heads(q, k, q_weight, k_weight, positions, rope: Optional[Rope], eps=1e-6, hadamard=False, out=None):
     """RMS norm of every head row with a weight per element (None = ones), then conqur_rope_heads, in one pass (rope None: no rotation)."""
     stream = _here(q)
-    q_out, k_out = _outputs(q, k, out)
-    call = _heads_call(q, k, positions, rope, CONQUR_HEADS_HADAMARD if hadamard else 0, eps, q_weight, k_weight, q_out, k_out)
+    call, q_out, k_out = _heads_call(q, k, positions, rope, CONQUR_HEADS_HADAMARD if hadamard else 0, eps, q_weight, k_weight, out)
     rc = (_lib or load()).conqur_norm_rope_heads(call, stream)
     if rc != 0:
         raise ConqurError(rc, "conqur_norm_rope_heads")
@@ -554,12 +563,12 @@ def conqur_norm_rope_heads_backward(q_grad, k_grad, q, k, q_weight, k_weight, po
         raise ConqurError(-1, "conqur_norm_rope_backward_scratch_bytes")
     assert q_grad is not None and (k is None) == (k_grad is None)
     if scratch is None:
-        scratch = _torch.empty(need, dtype=_torch.uint8, device=q.device)
+        scratch = q.new_empty(need, dtype=_torch.uint8)
     assert scratch.dtype == _torch.uint8 and scratch.is_contiguous() and scratch.get_device() == q.get_device()
-    dq, dk = _outputs(q, k, out)
-    dw = _torch.empty((2, d), dtype=_torch.float32, device=q.device)
-    call = _heads_call(q, k, positions, rope, CONQUR_HEADS_HADAMARD if hadamard else 0, eps, q_weight, k_weight, dq, dk, q_grad, k_grad,
-                       dw.data_ptr(), 0 if k is None else dw.data_ptr() + 4 * d)
+    dw = q.new_empty((2, d), dtype=_torch.float32)
+    at = dw.data_ptr()
+    call, dq, dk = _heads_call(q, k, positions, rope, CONQUR_HEADS_HADAMARD if hadamard else 0, eps, q_weight, k_weight, out, q_grad, k_grad,
+                               at, 0 if k is None else at + 4 * d)
     rc = lib.conqur_norm_rope_heads_backward(call, scratch.data_ptr(), scratch.numel(), stream)
     if rc != 0:
         raise ConqurError(rc, "conqur_norm_rope_heads_backward")
@@ -593,13 +602,12 @@ class KVCache:
 def conqur_kv_append(cache: KVCache, k, v, slots) -> None:
     """Write keys and values (tokens, kv_heads, head_dim), bf16, into their slots (int64, one per token; negative: not stored)."""
     stream = _here(cache.data)
-    n = slots.shape[0]
-    shape = (n, cache.kv_heads, cache.head_dim)
-    assert slots.dtype == _torch.int64 and slots.dim() == 1 and slots.get_device() == cache._device and (n <= 1 or slots.stride(0) == 1)
-    for x in (k, v):
-        assert x.dtype == _torch.bfloat16 and x.shape == shape and x.get_device() == cache._device and x.stride(2) == 1
-    rc = (_lib or load()).conqur_kv_append(cache._ref, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                           n, slots.data_ptr(), stream)
+    (n,), bf16, dev = slots.shape, _torch.bfloat16, cache._device
+    ks, vs, shape = k.stride(), v.stride(), (n, cache.kv_heads, cache.head_dim)
+    assert slots.dtype is _torch.int64 and slots.get_device() == dev and (n <= 1 or slots.stride(0) == 1)
+    assert k.dtype is bf16 and k.shape == shape and k.get_device() == dev and ks[2] == 1
+    assert v.dtype is bf16 and v.shape == shape and v.get_device() == dev and vs[2] == 1
+    rc = (_lib or load()).conqur_kv_append(cache._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], n, slots.data_ptr(), stream)
     if rc != 0:
         raise ConqurError(rc, "conqur_kv_append")
 
@@ -607,9 +615,10 @@ def conqur_kv_append(cache: KVCache, k, v, slots) -> None:
 def conqur_kv_read(cache: KVCache, slots, dtype=None):
     """Keys and values (tokens, kv_heads, head_dim) that slots hold, as bf16 (default) or fp32; zeros for a negative slot."""
     stream = _here(cache.data)
-    n = slots.shape[0]
-    assert slots.dtype == _torch.int64 and slots.dim() == 1 and slots.get_device() == cache._device and (n <= 1 or slots.stride(0) == 1)
-    k, v = _torch.empty((2, n, cache.kv_heads, cache.head_dim), dtype=dtype or _torch.bfloat16, device=cache.data.device)
+    (n,) = slots.shape
+    assert slots.dtype is _torch.int64 and slots.get_device() == cache._device and (n <= 1 or slots.stride(0) == 1)
+    k = cache.data.new_empty((n, cache.kv_heads, cache.head_dim), dtype=dtype or _torch.bfloat16)
+    v = _torch.empty_like(k)
     rc = (_lib or load()).conqur_kv_read(cache._ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], stream)
     if rc != 0:
         raise ConqurError(rc, "conqur_kv_read")
@@ -655,18 +664,21 @@ def conqur_tree_attention(q, cache: KVCache, starts, contexts, table, mask=None,
         assert mask.dtype == t.int64 and mask.shape == (n,) and mask.is_contiguous() and mask.get_device() == dev
         mask_ptr = mask.data_ptr()
     if out is None:
-        out = t.empty((n, heads, d), dtype=t.bfloat16, device=q.device)
+        out = t.empty_like(q, memory_format=t.contiguous_format)
+    else:
+        assert out.dtype is t.bfloat16 and out.shape == q.shape and out.stride(2) == 1 and out.get_device() == dev
     if lse is None:
-        lse = t.empty((n, heads), dtype=t.float32, device=q.device)
-    assert out.dtype == t.bfloat16 and out.shape == q.shape and out.stride(2) == 1 and out.get_device() == dev
-    assert lse.dtype == t.float32 and lse.shape == (n, heads) and lse.get_device() == dev and (heads == 1 or lse.stride(1) == 1)
+        lse = q.new_empty((n, heads), dtype=t.float32)
+    else:
+        assert lse.dtype is t.float32 and lse.shape == (n, heads) and lse.get_device() == dev and (heads == 1 or lse.stride(1) == 1)
     if workspace is None:
         workspace = attention_workspace(cache, group, max_nodes)
     assert workspace.dtype == t.uint8 and workspace.is_contiguous() and workspace.get_device() == dev
+    qs, os, ts = q.stride(), out.stride(), table.stride()
     call = _TREE_CALL.pack(
-        _TREE_CALL.size, batch, group, max_nodes, d ** -0.5 if scale is None else scale, table.shape[1], n,
-        q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(), lse.stride(0),
-        starts.data_ptr(), contexts.data_ptr(), table.data_ptr(), table.stride(0), mask_ptr, workspace.data_ptr(), workspace.numel())
+        _TREE_CALL.size, batch, group, max_nodes, d ** -0.5 if scale is None else scale, table.shape[1], n, q.data_ptr(), qs[0], qs[1],
+        out.data_ptr(), os[0], os[1], lse.data_ptr(), lse.stride(0), starts.data_ptr(), contexts.data_ptr(), table.data_ptr(), ts[0], mask_ptr,
+        workspace.data_ptr(), workspace.numel())
     rc = (_lib or load()).conqur_tree_attention(cache._ref, call, stream)
     if rc != 0:
         raise ConqurError(rc, "conqur_tree_attention")

@@ -8,6 +8,9 @@
 //   - A head row of D elements lies in D/16 lanes, two 16-byte (bf16) pieces each, chosen so that both elements of every pair are in
 //     one lane: no exchange for the rotation, log2(D/16) exchanges for the norm's sum and for R_3 (log2 16 of its levels are
 //     inside a lane).
+//   - Arithmetic goes two fp32 at a time (f32x2).  A lane's sixteen elements are kept as the eight first and the eight second ones of its pairs, whatever the
+//     layout, so that a rotation is five packed operations for two pairs; a norm's factor comes last, where R_3's 1 / sqrt(d) is, and its weights lie in shared
+//     memory (in registers they would cost a quarter of the warps).
 //   - Angles: the table holds each frequency in turns per position as a 64-bit binary fraction.  position * fraction modulo 2^64 is the
 //     exact turn modulo 1 (one 64-bit product, no range reduction, any position), its top 32 bits go to sincospif.
 // Rows that do not fit that scheme (head_dim not a multiple of 16 or without an instance below, half-layout pairs that do not lie in
@@ -120,54 +123,145 @@ __device__ __forceinline__ float row_sum(float v, int l, int lane) {
   return __shfl_sync(0xffffffffu, v, lane - l);
 }
 
-// One row (or the matching one of the gradients), spread over D/16 lanes.
+// A row is spread over D/16 lanes.
 template <int D>
 struct Row {
   static constexpr int L = D / 16;                 // lanes a row takes
   static constexpr int PER_WARP = 32 / L;          // rows a warp works on side by side
 };
 
-template <int L>
-__device__ __forceinline__ void row_hadamard(float (&x)[16], int l, float scale) {
-#pragma unroll
-  for (int m = 1; m < 16; m <<= 1)
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (!(i & m)) {
-        const float a = x[i], b = x[i | m];
-        x[i] = a + b;
-        x[i | m] = a - b;
-      }
-#pragma unroll
-  for (int m = 1; m < L; m <<= 1) {
-    const float sgn = (l & m) ? -1.f : 1.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = fmaf(sgn, x[i], __shfl_xor_sync(0xffffffffu, x[i], m));
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] *= scale;
+// ---- two fp32 at a time
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 mk2(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ f2 mk2(float v) { return mk2(v, v); }
+__device__ __forceinline__ void get2(f2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 sub2(f2 a, f2 b) {
+  f2 r;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float sum2(f2 v) {
+  float a, b;
+  get2(v, a, b);
+  return a + b;
 }
 
-// Pairs whose bit in `turned` is clear stay as they are.
-__device__ __forceinline__ void row_rotate(float (&x)[16], const float (&c)[8], const float (&s)[8], float sign, int layout, uint32_t turned) {
-  if (layout == CONQUR_ROPE_HALF) {
-    if (turned) {
+// A lane's sixteen elements: the first and the second elements of its eight pairs.  HALF: its two pieces; else the even and odd elements of both.
+struct Pairs {
+  f2 a[4], b[4];
+};
+template <bool HALF>
+__device__ __forceinline__ Pairs pairs_of(const float (&x)[16]) {
+  Pairs p;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float a = x[i], b = x[8 + i], t = sign * s[i];
-        x[i] = fmaf(a, c[i], -b * t);
-        x[8 + i] = fmaf(a, t, b * c[i]);
+  for (int i = 0; i < 4; ++i) {
+    p.a[i] = HALF ? mk2(x[2 * i], x[2 * i + 1]) : mk2(x[4 * i], x[4 * i + 2]);
+    p.b[i] = HALF ? mk2(x[8 + 2 * i], x[8 + 2 * i + 1]) : mk2(x[4 * i + 1], x[4 * i + 3]);
+  }
+  return p;
+}
+template <bool HALF>
+__device__ __forceinline__ void pairs_to(const Pairs& p, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (HALF) {
+      get2(p.a[i], x[2 * i], x[2 * i + 1]);
+      get2(p.b[i], x[8 + 2 * i], x[8 + 2 * i + 1]);
+    } else {
+      get2(p.a[i], x[4 * i], x[4 * i + 2]);
+      get2(p.b[i], x[4 * i + 1], x[4 * i + 3]);
+    }
+  }
+}
+
+// Without the 1 / sqrt(d).  (The levels may come in any order, and so may the elements of a lane.)
+template <int L>
+__device__ __forceinline__ void row_hadamard(Pairs& x, int l) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f2 s = add2(x.a[i], x.b[i]), d = sub2(x.a[i], x.b[i]);
+    x.a[i] = s;
+    x.b[i] = d;
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    f2* v = k ? x.b : x.a;
+#pragma unroll
+    for (int m = 1; m < 4; m <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!(i & m)) {
+          const f2 s = add2(v[i], v[i | m]), d = sub2(v[i], v[i | m]);
+          v[i] = s;
+          v[i | m] = d;
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      get2(v[i], lo, hi);
+      v[i] = mk2(lo + hi, lo - hi);
+    }
+#pragma unroll
+    for (int m = 1; m < L; m <<= 1) {
+      const f2 sgn = mk2((l & m) ? -1.f : 1.f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        get2(v[i], lo, hi);
+        lo = __shfl_xor_sync(0xffffffffu, lo, m);
+        hi = __shfl_xor_sync(0xffffffffu, hi, m);
+        v[i] = fma2(sgn, v[i], mk2(lo, hi));
       }
     }
-  } else {
+  }
+}
+
+// Pairs that do not turn keep to their own element (a sine of 0 would let what is not finite over); their cosine is the scale.
+template <bool HALF>
+__device__ __forceinline__ void row_spin(Pairs& x, const f2 (&c)[4], const f2 (&s)[4], uint32_t turned) {
+  if (HALF && !turned) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float a = x[2 * i], b = x[2 * i + 1], t = sign * s[i];
-      if (turned & (1u << i)) {
-        x[2 * i] = fmaf(a, c[i], -b * t);
-        x[2 * i + 1] = fmaf(a, t, b * c[i]);
-      }
+    for (int i = 0; i < 4; ++i) {
+      x.a[i] = mul2(x.a[i], c[i]);
+      x.b[i] = mul2(x.b[i], c[i]);
     }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f2 a = x.a[i], b = x.b[i];
+    f2 u = sub2(mul2(a, c[i]), mul2(b, s[i])), v = fma2(a, s[i], mul2(b, c[i]));
+    if (!HALF && turned != 0xFFu) {
+      float u0, u1, v0, v1, a0, a1, b0, b1;
+      get2(u, u0, u1);
+      get2(v, v0, v1);
+      get2(mul2(a, c[i]), a0, a1);
+      get2(mul2(b, c[i]), b0, b1);
+      const bool y = turned & (1u << (2 * i)), z = turned & (2u << (2 * i));
+      u = mk2(y ? u0 : a0, z ? u1 : a1);
+      v = mk2(y ? v0 : b0, z ? v1 : b1);
+    }
+    x.a[i] = u;
+    x.b[i] = v;
   }
 }
 
@@ -218,20 +312,41 @@ __device__ __forceinline__ void token_of(const HeadsArgs& a, int64_t t, int64_t&
   }
 }
 
-__device__ __forceinline__ void lane_angles(const HeadsArgs& a, int64_t b, int64_t t, const LanePlan& q, float (&c)[8], float (&s)[8]) {
-  if (!q.turned) return;
-  const unsigned long long pos = (unsigned long long)a.pos[b * a.pos_b + t];
-  const float amp = (float)__longlong_as_double((long long)a.table[a.rot >> 1]);
+// cos and sin of the lane's eight pairs (times the amplitude; the sine times `sign`); 1 and 0 where they do not turn.
+__device__ __forceinline__ void lane_angles(const HeadsArgs& a, int64_t b, int64_t t, const LanePlan& q, float sign, f2 (&c)[4], f2 (&s)[4]) {
+  float cf[8], sf[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (q.turned & (1u << i)) angle(pos, a.table[q.f[i >> 2] + (i & 3)], amp, c[i], s[i]);
+  for (int i = 0; i < 8; ++i) {
+    cf[i] = 1.f;
+    sf[i] = 0.f;
+  }
+  if (q.turned) {
+    const unsigned long long pos = (unsigned long long)a.pos[b * a.pos_b + t];
+    const float amp = (float)__longlong_as_double((long long)a.table[a.rot >> 1]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (q.turned & (1u << i)) {
+        angle(pos, a.table[q.f[i >> 2] + (i & 3)], amp, cf[i], sf[i]);
+        sf[i] *= sign;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    c[i] = mk2(cf[2 * i], cf[2 * i + 1]);
+    s[i] = mk2(sf[2 * i], sf[2 * i + 1]);
+  }
 }
 
 // Forward (and conqur_rope_heads' inverse).  Warp w of block x works on token HEADS_WARPS x + w; block row y of gridDim.y takes every gridDim.y-th group of
-// Row<D>::PER_WARP heads (more than one only where the tokens alone would leave the GPU idle).
-template <typename T, int D, bool NORM>
-__global__ void __launch_bounds__(HEADS_THREADS) heads_kernel(const HeadsArgs a) {
+// Row<D>::PER_WARP heads (more than one only where the tokens alone would leave the GPU idle).  Two groups travel while one is worked on.
+template <typename T, int D, bool NORM, bool HALF>
+__global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 6 : 5) heads_kernel(const HeadsArgs a) {
   constexpr int L = Row<D>::L, PW = Row<D>::PER_WARP;
+  __shared__ __align__(16) float weight[NORM ? 2 * D : 4];
+  if (NORM) {
+    for (int e = threadIdx.x; e < 2 * D; e += HEADS_THREADS) weight[e] = load_weight(a.seg[e >= D].weight, a.weight_bf16, e >= D ? e - D : e);
+    __syncthreads();
+  }
   const int lane = threadIdx.x & 31;
   const int row = lane / L, l = lane - row * L;
   const int64_t token = (int64_t)blockIdx.x * HEADS_WARPS + (threadIdx.x >> 5);
@@ -239,70 +354,98 @@ __global__ void __launch_bounds__(HEADS_THREADS) heads_kernel(const HeadsArgs a)
   int64_t b, t;
   token_of(a, token, b, t);
   const LanePlan q = lane_plan<D>(l, a.rot, a.layout);
-  const int nq = (a.seg[0].heads + PW - 1) / PW, total = nq + (a.seg[1].heads + PW - 1) / PW;
-
-  auto source = [&](int it, const T*& p) -> bool {
-    const HeadsPtr& g = a.seg[it >= nq];
-    const int h = (it >= nq ? it - nq : it) * PW + row;
-    p = static_cast<const T*>(g.in) + b * g.in_b + t * g.in_t + h * g.in_h;
-    return row < PW && h < g.heads;
-  };
-  Piece<T> r0, r1;
-  const T* p;
-  int it = blockIdx.y;
-  if (source(it, p)) {
-    r0.load(p + q.p0);
-    r1.load(p + q.p1);
-  }
-  float c[8], s[8];
-  lane_angles(a, b, t, q, c, s);
-  const float sign = a.inverse ? -1.f : 1.f;
-  float w[NORM ? 16 : 1];
-  int have = -1;
-  for (; it < total; it += gridDim.y) {
-    const int sg = it >= nq;
-    float x[16];
-    r0.get(x);
-    r1.get(x + 8);
-    const int next = it + gridDim.y;
-    if (next < total && source(next, p)) {                    // the next rows travel while these are worked on
-      r0.load(p + q.p0);
-      r1.load(p + q.p1);
-    }
-    if (NORM) {
-      if (have != sg) {
-        have = sg;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = load_weight(a.seg[sg].weight, a.weight_bf16, (i < 8 ? q.p0 : q.p1) + (i & 7));
-      }
-      float ss = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
-      ss = row_sum<L>(ss, l, lane);
-      const float rstd = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] *= rstd * w[i];
-    }
-    if (!NORM && a.inverse && a.hadamard) row_hadamard<L>(x, l, a.scale);
-    row_rotate(x, c, s, sign, a.layout, q.turned);
-    if (!(!NORM && a.inverse) && a.hadamard) row_hadamard<L>(x, l, a.scale);
+  const float scale = a.hadamard ? a.scale : 1.f;
+  const bool before = !NORM && a.inverse && a.hadamard, after = a.hadamard && !before;
+  const int nq = (a.seg[0].heads + PW - 1) / PW;
+  int at = blockIdx.y;                                         // this block row's next group, queries first
+  f2 c[4], s[4];
+  bool have = false;
+#pragma unroll 1
+  for (int sg = 0; sg < 2; ++sg) {
     const HeadsPtr& g = a.seg[sg];
-    const int h = (sg ? it - nq : it) * PW + row;
-    if (row < PW && h < g.heads) {
-      T* o = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + h * g.out_h;
-      Piece<T>::store(o + q.p0, x);
-      Piece<T>::store(o + q.p1, x + 8);
+    const int groups = (g.heads + PW - 1) / PW;
+    int it = sg ? at - nq : at;
+    if (it >= groups) continue;
+    const int64_t in_step = (int64_t)gridDim.y * PW * g.in_h, out_step = (int64_t)gridDim.y * PW * g.out_h;
+    int h = it * PW + row;
+    const int heads = row < PW ? g.heads : 0, h_step = gridDim.y * PW;
+    const T* p = static_cast<const T*>(g.in) + b * g.in_b + t * g.in_t + h * g.in_h;
+    T* o = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + h * g.out_h;
+    Piece<T> r[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (h + k * h_step < heads) {
+        r[k][0].load(p + k * in_step + q.p0);
+        r[k][1].load(p + k * in_step + q.p1);
+      }
+    if (!have) {
+      lane_angles(a, b, t, q, a.inverse ? -1.f : 1.f, c, s);
+      have = true;
     }
+    int k = 0;
+#pragma unroll 2
+    for (; it < groups; it += gridDim.y, k ^= 1) {
+      float v[16];
+      r[k][0].get(v);
+      r[k][1].get(v + 8);
+      Pairs x = pairs_of<HALF>(v);
+      if (h + 2 * h_step < heads) {
+        r[k][0].load(p + 2 * in_step + q.p0);
+        r[k][1].load(p + 2 * in_step + q.p1);
+      }
+      float f = scale;
+      if (NORM) {
+        f2 ss = mul2(x.a[0], x.a[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) ss = fma2(x.a[i], x.a[i], ss);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ss = fma2(x.b[i], x.b[i], ss);
+        f *= rsqrtf(fmaf(row_sum<L>(sum2(ss), l, lane), 1.f / D, a.eps));
+      }
+      if (before) row_hadamard<L>(x, l);
+      if (NORM) {
+        Piece<float> w0, w1;
+        w0.load(weight + sg * D + q.p0);
+        w1.load(weight + sg * D + q.p1);
+        w0.get(v); w1.get(v + 8);
+        const Pairs w = pairs_of<HALF>(v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x.a[i] = mul2(x.a[i], w.a[i]);
+          x.b[i] = mul2(x.b[i], w.b[i]);
+        }
+      }
+      row_spin<HALF>(x, c, s, q.turned);
+      if (after) row_hadamard<L>(x, l);
+      if (NORM || a.hadamard) {
+        const f2 f2v = mk2(f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x.a[i] = mul2(x.a[i], f2v);
+          x.b[i] = mul2(x.b[i], f2v);
+        }
+      }
+      if (h < heads) {
+        pairs_to<HALF>(x, v);
+        Piece<T>::store(o + q.p0, v);
+        Piece<T>::store(o + q.p1, v + 8);
+      }
+      p += in_step;
+      o += out_step;
+      h += h_step;
+    }
+    at = sg ? at : it;                                         // the keys' groups go on in the same stride
   }
 }
 
 // Backward of the normed form.  With g = the gradient taken back through R_3 and the rotation, r = 1 / sqrt(mean x^2 + eps):
-//   dw = sum over rows of g * x r        dx = r (w g - x r^2 mean(w g x))
+//   dw = sum over rows of g * x r        dx = r w g - x r (r^2 mean(w g x))
 // A block works on the queries or on the keys; its warps walk tokens and keep their share of dw in registers.
-template <typename T, int D>
-__global__ void __launch_bounds__(HEADS_THREADS) heads_grad_kernel(const HeadsArgs a) {
+template <typename T, int D, bool HALF>
+__global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 4 : 3) heads_grad_kernel(const HeadsArgs a) {
   constexpr int L = Row<D>::L, PW = Row<D>::PER_WARP;
   __shared__ float sums[HEADS_WARPS][D];
+  __shared__ __align__(16) float weight[D];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = lane / L, l = lane - row * L;
   const int sg = (int)blockIdx.x >= a.q_blocks;
@@ -310,12 +453,12 @@ __global__ void __launch_bounds__(HEADS_THREADS) heads_grad_kernel(const HeadsAr
   const HeadsPtr& g = a.seg[sg];
   const LanePlan q = lane_plan<D>(l, a.rot, a.layout);
   const int total = (g.heads + PW - 1) / PW;
-  float w[16], dw[16];
+  const float scale = a.hadamard ? a.scale : 1.f;
+  Pairs dw;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    w[i] = load_weight(g.weight, a.weight_bf16, (i < 8 ? q.p0 : q.p1) + (i & 7));
-    dw[i] = 0.f;
-  }
+  for (int i = 0; i < 4; ++i) dw.a[i] = dw.b[i] = 0ull;
+  for (int e = threadIdx.x; e < D; e += HEADS_THREADS) weight[e] = load_weight(g.weight, a.weight_bf16, e);
+  __syncthreads();
   for (int64_t token = (int64_t)blk * HEADS_WARPS + warp; token < a.n; token += (int64_t)blocks * HEADS_WARPS) {
     int64_t b, t;
     token_of(a, token, b, t);
@@ -323,54 +466,81 @@ __global__ void __launch_bounds__(HEADS_THREADS) heads_grad_kernel(const HeadsAr
     const T* yp = static_cast<const T*>(g.grad) + b * g.grad_b + t * g.grad_t + row * g.grad_h;
     T* op = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + row * g.out_h;
     Piece<T> x0, x1, y0, y1;
-    bool mine = row < PW && row < g.heads;
-    auto fetch = [&](int it) {
-      x0.load(xp + it * PW * g.in_h + q.p0);
-      x1.load(xp + it * PW * g.in_h + q.p1);
-      y0.load(yp + it * PW * g.grad_h + q.p0);
-      y1.load(yp + it * PW * g.grad_h + q.p1);
+    int h = row;
+    const int heads = row < PW ? g.heads : 0;
+    auto fetch = [&]() {
+      x0.load(xp + q.p0);
+      x1.load(xp + q.p1);
+      y0.load(yp + q.p0);
+      y1.load(yp + q.p1);
     };
-    if (mine) fetch(0);
-    float c[8], s[8];
-    lane_angles(a, b, t, q, c, s);
+    if (h < heads) fetch();
+    f2 c[4], s[4];
+    lane_angles(a, b, t, q, -1.f, c, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      c[i] = mul2(c[i], mk2(scale));
+      s[i] = mul2(s[i], mk2(scale));
+    }
+#pragma unroll 1
     for (int it = 0; it < total; ++it) {
-      float x[16], y[16];
-      x0.get(x); x1.get(x + 8);
-      y0.get(y); y1.get(y + 8);
-      const bool now = mine;
-      mine = row < PW && (it + 1) * PW + row < g.heads;
-      if (it + 1 < total && mine) fetch(it + 1);
-      if (a.hadamard) row_hadamard<L>(y, l, a.scale);
-      row_rotate(y, c, s, -1.f, a.layout, q.turned);
-      float ss = 0.f, sx = 0.f;
+      float v[16];
+      x0.get(v); x1.get(v + 8);
+      Pairs x = pairs_of<HALF>(v);
+      y0.get(v); y1.get(v + 8);
+      Pairs y = pairs_of<HALF>(v);
+      const bool now = h < heads;
+      h += PW;
+      xp += PW * g.in_h;
+      yp += PW * g.grad_h;
+      if (h < heads) fetch();
+      if (a.hadamard) row_hadamard<L>(y, l);
+      row_spin<HALF>(y, c, s, q.turned);
+      Piece<float> w0, w1;                                     // (shared memory: sixteen registers less)
+      w0.load(weight + q.p0);
+      w1.load(weight + q.p1);
+      w0.get(v); w1.get(v + 8);
+      const Pairs w = pairs_of<HALF>(v);
+      f2 ss = mul2(x.a[0], x.a[0]), sx = 0ull;
+      Pairs wy;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        ss = fmaf(x[i], x[i], ss);
-        sx = fmaf(w[i] * y[i], x[i], sx);
+      for (int i = 0; i < 4; ++i) {
+        if (i) ss = fma2(x.a[i], x.a[i], ss);
+        ss = fma2(x.b[i], x.b[i], ss);
+        wy.a[i] = mul2(w.a[i], y.a[i]);
+        wy.b[i] = mul2(w.b[i], y.b[i]);
+        sx = fma2(wy.a[i], x.a[i], sx);
+        sx = fma2(wy.b[i], x.b[i], sx);
       }
-      ss = row_sum<L>(ss, l, lane);
-      sx = row_sum<L>(sx, l, lane);
-      const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-      const float k = sx * (1.f / D) * r * r;
+      const float r = rsqrtf(fmaf(row_sum<L>(sum2(ss), l, lane), 1.f / D, a.eps));
+      const float k = -row_sum<L>(sum2(sx), l, lane) * (1.f / D) * r * r;
       if (now) {
+        const f2 r2 = mk2(r), k2 = mk2(k);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float u = x[i] * r;
-          dw[i] = fmaf(y[i], u, dw[i]);
-          y[i] = r * fmaf(w[i], y[i], -x[i] * k);
+        for (int i = 0; i < 4; ++i) {
+          x.a[i] = mul2(x.a[i], r2);
+          x.b[i] = mul2(x.b[i], r2);
+          dw.a[i] = fma2(y.a[i], x.a[i], dw.a[i]);
+          dw.b[i] = fma2(y.b[i], x.b[i], dw.b[i]);
+          y.a[i] = fma2(x.a[i], k2, mul2(wy.a[i], r2));
+          y.b[i] = fma2(x.b[i], k2, mul2(wy.b[i], r2));
         }
-        Piece<T>::store(op + it * PW * g.out_h + q.p0, y);
-        Piece<T>::store(op + it * PW * g.out_h + q.p1, y + 8);
+        pairs_to<HALF>(y, v);
+        Piece<T>::store(op + q.p0, v);
+        Piece<T>::store(op + q.p1, v + 8);
       }
+      op += PW * g.out_h;
     }
   }
   // rows of the warp, then warps of the block, in a fixed order
+  float d[16];
+  pairs_to<HALF>(dw, d);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    float v = dw[i];
+    float v = d[i];
 #pragma unroll
     for (int j = 1; j < PW; ++j) {
-      const float o = __shfl_sync(0xffffffffu, dw[i], (j * L + l) & 31);
+      const float o = __shfl_sync(0xffffffffu, d[i], (j * L + l) & 31);
       v += o;
     }
     if (row == 0) sums[warp][(i < 8 ? q.p0 : q.p1) + (i & 7)] = v;
@@ -696,7 +866,8 @@ int forward(const HeadsArgs& a, bool vec, cudaStream_t s) {
       constexpr int D = decltype(d)::value, PW = Row<D>::PER_WARP;
       const int total = (a.seg[0].heads + PW - 1) / PW + (a.seg[1].heads + PW - 1) / PW;
       const int split = (int)(want < total ? want : total);
-      heads_kernel<T, D, NORM><<<dim3((unsigned)blocks, split), HEADS_THREADS, 0, s>>>(a);
+      if (a.layout == CONQUR_ROPE_HALF && a.rot) heads_kernel<T, D, NORM, true><<<dim3((unsigned)blocks, split), HEADS_THREADS, 0, s>>>(a);
+      else heads_kernel<T, D, NORM, false><<<dim3((unsigned)blocks, split), HEADS_THREADS, 0, s>>>(a);
     });
   if (!done) {
     const int most = a.seg[0].heads > a.seg[1].heads ? a.seg[0].heads : a.seg[1].heads;
@@ -713,7 +884,7 @@ int backward(HeadsArgs a, bool vec, float* dq, float* dk, cudaStream_t s) {
   int qb = 0, kb = 0;
   if (a.n > 0) {
     // as many blocks as stay resident, shared out in proportion to the heads; fewer where there are few tokens
-    const int most = sms * 4 < GRAD_BLOCKS_MAX ? sms * 4 : GRAD_BLOCKS_MAX;
+    const int most = sms * (sizeof(T) == 2 ? 4 : 3) < GRAD_BLOCKS_MAX ? sms * (sizeof(T) == 2 ? 4 : 3) : GRAD_BLOCKS_MAX;
     const int64_t each = (a.n + HEADS_WARPS - 1) / HEADS_WARPS;
     const int hq = a.seg[0].heads, hk = a.seg[1].heads;
     kb = hk ? (int)((int64_t)most * hk / (hq + hk)) : 0;
@@ -725,7 +896,10 @@ int backward(HeadsArgs a, bool vec, float* dq, float* dk, cudaStream_t s) {
     a.q_blocks = qb;
     bool done = false;
     if (vec)
-      done = with_dim(a.head_dim, [&](auto d) { heads_grad_kernel<T, decltype(d)::value><<<qb + kb, HEADS_THREADS, 0, s>>>(a); });
+      done = with_dim(a.head_dim, [&](auto d) {
+        if (a.layout == CONQUR_ROPE_HALF && a.rot) heads_grad_kernel<T, decltype(d)::value, true><<<qb + kb, HEADS_THREADS, 0, s>>>(a);
+        else heads_grad_kernel<T, decltype(d)::value, false><<<qb + kb, HEADS_THREADS, 0, s>>>(a);
+      });
     if (!done) heads_general_kernel<T, MODE_GRAD><<<qb + kb, HEADS_THREADS, general_smem(a), s>>>(a);
     const int rc = launched();
     if (rc != CONQUR_OK) return rc;
