@@ -39,7 +39,7 @@ struct AttnArgs {
   int* flags;
 };
 
-enum { KV_FLAG_BAD_INDEX = 1 };
+enum { KV_FLAG_BAD_INDEX = 1, KV_FLAG_TIMEOUT = 2 };
 
 constexpr int ATTN_UNIT = 64;                                    // tokens: what the work is counted and cut in, a multiple of the largest page
 

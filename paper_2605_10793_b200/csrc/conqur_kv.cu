@@ -15,6 +15,7 @@
 
 #include "../../include/conqur.h"
 #include "conqur_attention.cuh"
+#include "conqur_attention_tc.cuh"
 
 using namespace conqur;
 using bf16 = __nv_bfloat16;
@@ -275,14 +276,19 @@ int rows_args(const conqur_kv_cache* c, int64_t n, const int64_t* slots, RowsArg
 
 struct AttnVariant {
   void (*kernel)(const kv::AttnArgs);
-  int rows, threads, smem, slot_floats;
+  int rows, threads, smem, slot_floats, ctas_max;
+  float code_scale;                       // 4 bits: what the scores' units ask for
 };
 template <typename C>
 AttnVariant variant() {
-  return {kv::attn_kernel<C>, C::ROWS, C::THREADS, C::SMEM, C::PART * 32};
+  return {kv::attn_kernel<C>, C::ROWS, C::THREADS, C::SMEM, C::PART * 32, 592, C::BITS == 4 ? kv::ATTN_Q_BACK : 1.f};
+}
+template <typename C>
+AttnVariant tree_variant() {
+  return {kv::attn_tree_kernel<C>, C::ROWS, C::THREADS, C::SMEM, C::SLOT, 160, C::BITS == 4 ? 64.f : 1.f};
 }
 constexpr int ATTN_VARIANTS = 3;
-constexpr int ATTN_CTAS_MAX = 592;        // runs of work: 4 per SM
+constexpr int ATTN_CTAS_MAX = 592;        // runs of work: 4 per SM (the tensor cores' variant: 1, and larger parts)
 constexpr size_t ATTN_COUNTER_BYTES = (ATTN_CTAS_MAX * sizeof(unsigned) + 255) / 256 * 256;      // at the workspace's start in every call
 
 template <int BITS, int D>
@@ -293,10 +299,10 @@ AttnVariant by_rows(int i) {
   switch (i) {
     case 0: return variant<kv::AttnCfg<BITS, D, 1, small ? 8 : 4, (small ? 2 : 3) * halves, small ? 2 : 1>>();
     case 1: return variant<kv::AttnCfg<BITS, D, 2, small ? 8 : 4, (small ? 4 : 2) * halves, 1>>();
-    default: return variant<kv::AttnCfg<BITS, D, 4, small ? 8 : 4, 2 * halves, 1>>();
+    default: return tree_variant<kv::TreeCfg<BITS, D>>();
   }
 }
-// The fewest rows that hold a sequence's, or blocks of 32.
+// Eight or sixteen rows on the warps' own products, more on the tcgen05 tensor cores in blocks of 128.
 int rows_class(int rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : 2; }
 AttnVariant pick(int bits, int d, int cls) {
   if (bits == 4) return d == 64 ? by_rows<4, 64>(cls) : by_rows<4, 128>(cls);
@@ -385,17 +391,18 @@ extern "C" int conqur_kv_status(void* cuda_stream) {
   int f = 0;
   if (!flags || cudaMemcpyAsync(&f, flags, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) return CONQUR_ERR_CUDA;
   if (f && (cudaMemsetAsync(flags, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)) return CONQUR_ERR_CUDA;
-  return (f & kv::KV_FLAG_BAD_INDEX) ? CONQUR_ERR_BAD_INDEX : CONQUR_OK;
+  return (f & kv::KV_FLAG_TIMEOUT) ? CONQUR_ERR_TIMEOUT : (f & kv::KV_FLAG_BAD_INDEX) ? CONQUR_ERR_BAD_INDEX : CONQUR_OK;
 }
 
 extern "C" size_t conqur_tree_attention_workspace_bytes(const conqur_kv_cache* cache, int32_t group, int32_t max_nodes) {
   if (!attn_sizes_ok(cache, 0, group, max_nodes)) return 0;
   size_t most = 0;                         // the variants of fewer rows may have the larger slots
   for (int i = 0; i <= rows_class(group * max_nodes); ++i) {
-    const size_t n = pick(cache->bits, cache->head_dim, i).slot_floats;
+    const AttnVariant v = pick(cache->bits, cache->head_dim, i);
+    const size_t n = (size_t)2 * v.ctas_max * v.slot_floats;
     if (n > most) most = n;
   }
-  return ATTN_COUNTER_BYTES + (size_t)2 * ATTN_CTAS_MAX * most * sizeof(float);
+  return ATTN_COUNTER_BYTES + most * sizeof(float);
 }
 
 extern "C" int conqur_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* c, void* cuda_stream) {
@@ -423,7 +430,7 @@ extern "C" int conqur_tree_attention(const conqur_kv_cache* cache, const conqur_
   a.block_bytes = block_bytes(cache); a.page_bytes = a.block_bytes * cache->kv_heads;
   a.codes_bytes = cache->page_size * cache->head_dim / 2; a.plane_bytes = cache->page_size * 128;
   a.rows = c->rows;
-  a.scale = (float)((double)c->scale * 1.4426950408889634) * (cache->bits == 4 ? kv::ATTN_Q_BACK : 1.f);
+  a.scale = (float)((double)c->scale * 1.4426950408889634) * v.code_scale;
   a.q = static_cast<const bf16*>(c->q_dev); a.q_t = c->q_token_stride; a.q_h = c->q_head_stride;
   a.out = static_cast<bf16*>(c->out_dev); a.o_t = c->out_token_stride; a.o_h = c->out_head_stride;
   a.lse = c->lse_dev; a.lse_t = c->lse_token_stride;
@@ -450,7 +457,7 @@ extern "C" int conqur_tree_attention(const conqur_kv_cache* cache, const conqur_
           cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return CONQUR_ERR_CUDA;
       if (per_sm < 1) return CONQUR_ERR_UNSUPPORTED;
-      f.ctas = per_sm * sms < ATTN_CTAS_MAX ? per_sm * sms : ATTN_CTAS_MAX;
+      f.ctas = per_sm * sms < v.ctas_max ? per_sm * sms : v.ctas_max;
       f.known = 1;
     }
     ctas = f.ctas;
