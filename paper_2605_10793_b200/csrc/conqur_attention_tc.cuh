@@ -1,11 +1,12 @@
 // The attention of conqur_attention.cuh for more than 16 query rows a key head (trees of drafted tokens): there the products set the pace, and they go to
 // the tcgen05 tensor cores.  One CTA an SM works on blocks of 128 rows, 64 tokens at a time:
-//   S = Q K^T (128 x 64) and O += P V (128 x D) with accumulators in TMEM; S and P have two buffers, so that the products of one tile run
-//   while the exponentials of the other are taken.
-//   warps 0-3   one row a thread: scores from TMEM, bound, exponentials (no exchange between threads), P as bf16 to shared memory
-//   warps 4-7   bring keys and values: bf16 as they lie (the cache's planes are the operands' swizzled layout), codes turned into the bf16 integers
-//               (code - zero-point) / 64, exactly; the steps go to the scores and the probabilities
-//   warp 8      issues the products
+//   S = Q K^T (128 x 64) and O += P V (128 x D) with accumulators in TMEM, and so are Q and P: shared memory, which the products read their other operand
+//   from, is what is scarce here.  Tiles of even and odd number are two streams, each with its own S, P, O, bounds and sums, joined at the end of an
+//   item, so that two groups of warps take exponentials while the products of the other's tile run:
+//   warps 0-3, 4-7  one row a thread: scores from TMEM, bound, exponentials (no exchange between threads), P as bf16 to TMEM
+//   warps 8-11      bring keys and values into four stages: bf16 as they lie (the cache's planes are the operands' swizzled layout), codes turned into the
+//                   bf16 integers (code - zero-point) / 64, exactly; the steps go to the scores and the probabilities
+//   warp 12         issues the products: the scores of a stream's next tile as soon as those of the present one are read
 // The bound of a row is raised only when a score exceeds it by 2^8; then its accumulators are read, scaled and written back.  Work is cut into runs and parts
 // are joined as in conqur_attention.cuh.  Every wait between the warps is bounded: when one runs out the CTA latches TIMEOUT, writes nothing more and ends.
 // Floor of the exponentials: 8192 a tile at 16 a cycle, 512 cycles; the products take about the same.
@@ -18,20 +19,23 @@ namespace kv {
 template <int BITS_, int D_>
 struct TreeCfg {
   static constexpr int BITS = BITS_, D = D_;
-  static constexpr int ROWS = 128, THREADS = 288, PLANES = D / 64;
-  static constexpr int Q_BYTES = PLANES * 16384;               // 128 rows x 128 bytes a plane
+  static constexpr int ROWS = 128, THREADS = 416, PLANES = D / 64, STAGES = 4;
   static constexpr int T_BYTES = PLANES * 8192;                // keys or values of a tile
-  static constexpr int P_BYTES = 16384;
-  static constexpr int AUX_BYTES = 2048;
-  static constexpr int SMEM = 1024 + Q_BYTES + 4 * T_BYTES + 2 * P_BYTES + AUX_BYTES;
+  static constexpr int RAW = BITS == 4 ? 4 : 0, RAW_BYTES = 9216;   // tiles of codes on their way: 64 bytes and two records a thread
+  static constexpr int AUX_BYTES = 5120;
+  static constexpr int SMEM = 1024 + 2 * STAGES * T_BYTES + RAW * RAW_BYTES + AUX_BYTES;
+  // TMEM columns: scores 2 x 64, accumulators 2 x 128, the rows D / 2 (two bf16 a column), probabilities 2 x 32
+  static constexpr int T_O = 128, T_Q = 384, T_P = 448;
+  static_assert(SMEM <= 227 * 1024, "shared memory of an SM");
   static constexpr int SLOT = (D + 2) * 128;                   // floats of a part: columns of 128 rows; then bounds, sums
 };
 
 template <typename C>
 struct TreeAux {
-  uint64_t full[2], scored[2], ready[2], done[2];              // tile brought; S complete; P written; P V complete
-  float kstep[2][64], vstep[2][64];
-  uint32_t bad[2][2];                                          // tokens of a tile whose page could not be read
+  uint64_t full[C::STAGES], empty[C::STAGES], scored[2], read[2], ready[2], done[2];   // tile brought, free again; S complete, read; P written; P V complete
+  float kstep[C::STAGES][64], vstep[C::STAGES][64];
+  uint32_t bad[C::STAGES][2];                                  // tokens of a tile whose page could not be read
+  float bound[2][128], sum[2][128];                            // of the two streams
   Walk<C> w;
   uint32_t tmem;
   int abort_flag, last, odd;                                   // odd: some value near the end of the sequence is not finite
@@ -54,6 +58,15 @@ __device__ __forceinline__ void tmem_write16(uint32_t taddr, const uint32_t (&w)
         "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
       : "memory");
 }
+// D(tmem) (+)= A(tmem: lane = row, two consecutive k a column) B(smem)
+__device__ __forceinline__ void umma_from_tmem(uint32_t leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(leader)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_write_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
@@ -70,7 +83,7 @@ __device__ __forceinline__ uint4 codes8(uint32_t w, uint32_t bias) {
 __device__ __forceinline__ uint32_t zero_bias(uint32_t rec) { return fma_bf16x2(zero_of(rec) * 0x10001u, 0xFF00FF00u, 0x80008000u); }   // -z / 64
 __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
-// ---- warps 4-7: a thread takes a token's 64 dimensions of one plane, of keys and values (D = 64: threads 0-63 the keys, 64-127 the values)
+// ---- warps 8-11: a thread takes a token's 64 dimensions of one plane, of keys and values (D = 64: threads 0-63 the keys, 64-127 the values)
 template <typename C>
 struct Bring {
   int tok, plane;
@@ -78,10 +91,8 @@ struct Bring {
   const int* table;
   const uint8_t* head;
   int len;
-  int page, cur;                     // of the tile after next (asked for ahead), of the next tile
-  uint4 k[2], v[2];                  // 4 bits: the next tile's codes and records
-  uint32_t kr, vr;
-  bool good;
+  int page, later, cur;              // of the next tile to fetch and of the one after (asked for two ahead); 16 bits: of the one being brought
+  uint32_t goods;                    // a bit a slot of the ring: the page could be read
 
   __device__ __forceinline__ void item(const AttnArgs& a, const Walk<C>& w, int tid) {
     tok = tid & 63;
@@ -93,83 +104,92 @@ struct Bring {
     head = a.cache + (long long)(w.item % a.kv_heads) * a.block_bytes;
     len = w.s.context + w.s.nodes;
   }
-  __device__ __forceinline__ void ask(const AttnArgs& a, int tile, int end) {
+  __device__ __forceinline__ int look(const AttnArgs& a, int tile, int end) const {
     const int pos = tile * ATTN_UNIT + tok;
-    page = -1;
-    if (tile < end && pos < len && (pos >> a.log_page) < a.table_width) page = table[pos >> a.log_page];
+    return tile < end && pos < len && (pos >> a.log_page) < a.table_width ? table[pos >> a.log_page] : -1;
+  }
+  // The page of `tile` moves up, that of the one after is asked for.
+  __device__ __forceinline__ void ask(const AttnArgs& a, int tile, int end) {
+    page = later;
+    later = look(a, tile + 1, end);
   }
   __device__ __forceinline__ const uint8_t* block(const AttnArgs& a) const { return head + (long long)cur * a.page_bytes; }
-  // 4 bits: the codes of the tile whose page was asked for
-  __device__ __forceinline__ void load(const AttnArgs& a, int tile) {
-    cur = page;
-    good = (unsigned)cur < (unsigned)a.pages;
-    kr = vr = 0u;
-    k[0] = k[1] = v[0] = v[1] = make_uint4(0u, 0u, 0u, 0u);
-    if (C::BITS == 4 && good) {
-      const int at = (tile * ATTN_UNIT + tok) & (a.page_size - 1);
-      const uint8_t* p = block(a);
-      const uint8_t* c = p + at * (C::D / 2) + plane * 32;
-      if (keys) {
-        k[0] = *reinterpret_cast<const uint4*>(c);
-        k[1] = *reinterpret_cast<const uint4*>(c + 16);
-        kr = *reinterpret_cast<const uint32_t*>(p + 2 * a.codes_bytes + at * 4);
-      }
-      if (values) {
-        v[0] = *reinterpret_cast<const uint4*>(c + a.codes_bytes);
-        v[1] = *reinterpret_cast<const uint4*>(c + a.codes_bytes + 16);
-        vr = *reinterpret_cast<const uint32_t*>(p + 2 * a.codes_bytes + (a.page_size + at) * 4);
-      }
+  // 4 bits: the codes of the tile whose page was asked for, into this thread's places of a slot (zeros where there is no page)
+  __device__ __forceinline__ void fetch(const AttnArgs& a, uint8_t* raw, int slot, int tile, int tid) {
+    const bool good = (unsigned)page < (unsigned)a.pages;
+    goods = (goods & ~(1u << slot)) | ((good ? 1u : 0u) << slot);
+    const int at = (tile * ATTN_UNIT + tok) & (a.page_size - 1), n = good ? 16 : 0;
+    const uint8_t* p = head + (good ? (long long)page * a.page_bytes : 0);
+    const uint8_t* c = p + at * (C::D / 2) + plane * 32;
+    const uint32_t to = ptx::smem_u32(raw + slot * C::RAW_BYTES) + tid * 16;
+    if (keys) {
+      copy16(to, c, n);
+      copy16(to + 2048, c + 16, n);
     }
+    if (values) {
+      copy16(to + 4096, c + a.codes_bytes, n);
+      copy16(to + 6144, c + a.codes_bytes + 16, n);
+    }
+    const uint32_t rec = ptx::smem_u32(raw + slot * C::RAW_BYTES) + 8192 + tid * 8;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(rec), "l"(p + 2 * a.codes_bytes + at * 4), "r"(n / 4) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(rec + 4), "l"(p + 2 * a.codes_bytes + (a.page_size + at) * 4), "r"(n / 4) : "memory");
   }
-  static __device__ __forceinline__ void spread(uint8_t* row, const uint4 (&c)[2], uint32_t bias, int t) {
-    const uint32_t w[8] = {c[0].x, c[0].y, c[0].z, c[0].w, c[1].x, c[1].y, c[1].z, c[1].w};
+  static __device__ __forceinline__ void spread(uint8_t* row, const uint4 c0, const uint4 c1, uint32_t bias, int t) {
+    const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(row + ((i ^ (t & 7)) << 4)) = codes8(w[i], bias);
   }
-  __device__ __forceinline__ void put(const AttnArgs& a, TreeAux<C>* aux, uint8_t* tile_mem, int buf, int tile, int context) {
-    const int pos = tile * ATTN_UNIT + tok;
+  __device__ __forceinline__ void lost(const AttnArgs& a, TreeAux<C>* aux, int st, int tile, bool good, int tid) {
+    const unsigned x = __ballot_sync(0xffffffffu, !good && tile * ATTN_UNIT + tok < len);
+    if (tid < 64 && (tid & 31) == 0) {
+      aux->bad[st][tid >> 5] = x;
+      if (x) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
+    }
+  }
+  __device__ __forceinline__ void put(const AttnArgs& a, TreeAux<C>* aux, uint8_t* tile_mem, const uint8_t* raw, int slot, int st, int tid) {
     uint8_t* kd = tile_mem + plane * 8192 + tok * 128;
     uint8_t* vd = kd + C::T_BYTES;
-    const unsigned lost = __ballot_sync(0xffffffffu, !good && pos < len);
-    const int tid = threadIdx.x - 128;
-    if (tid < 64 && (tid & 31) == 0) {
-      aux->bad[buf][tid >> 5] = lost;
-      if (lost) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
+    const uint8_t* from = raw + slot * C::RAW_BYTES + tid * 16;
+    const uint2 rec = *reinterpret_cast<const uint2*>(raw + slot * C::RAW_BYTES + 8192 + tid * 8);
+    // (a record that says NaN: the step carries it; its codes are codes)
+    if (keys) spread(kd, *reinterpret_cast<const uint4*>(from), *reinterpret_cast<const uint4*>(from + 2048), zero_bias(rec.x), tok);
+    if (values) spread(vd, *reinterpret_cast<const uint4*>(from + 4096), *reinterpret_cast<const uint4*>(from + 6144), zero_bias(rec.y), tok);
+    if (tid < 64) aux->kstep[st][tok] = step_of(rec.x) * a.scale;                // the scale has the 64 of the codes
+    else aux->vstep[st][tok] = step_of(rec.y) * 64.f;
+  }
+  // 16 bits: the copies of the next tile (one group), and what is left to do when they are there
+  __device__ __forceinline__ void copy(const AttnArgs& a, uint8_t* tile_mem, int tile) {
+    cur = page;
+    const bool good = (unsigned)cur < (unsigned)a.pages;
+    uint8_t* kd = tile_mem + plane * 8192 + tok * 128;
+    uint8_t* vd = kd + C::T_BYTES;
+    const int at = (tile * ATTN_UNIT + tok) & (a.page_size - 1), bytes = good ? 16 : 0;
+    const uint8_t* p = good ? block(a) + plane * a.plane_bytes + at * 128 : a.cache;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (keys) copy16(ptx::smem_u32(kd + i * 16), p + i * 16, bytes);
+      if (values) copy16(ptx::smem_u32(vd + i * 16), good ? p + C::PLANES * a.plane_bytes + i * 16 : p, bytes);
     }
-    if (C::BITS == 4) {
-      // (a record that says NaN: the step carries it; its codes are codes)
-      if (keys) spread(kd, k, zero_bias(kr), tok);
-      if (values) spread(vd, v, zero_bias(vr), tok);
-      if (tid < 64) aux->kstep[buf][tok] = step_of(kr) * a.scale;               // the scale has the 64 of the codes
-      if (values && (C::D == 64 || tid >= 64)) aux->vstep[buf][tok] = step_of(vr) * 64.f;
-    } else {
-      const int at = pos & (a.page_size - 1), bytes = good ? 16 : 0;
-      const uint8_t* p = good ? block(a) + plane * a.plane_bytes + at * 128 : a.cache;
+  }
+  __device__ __forceinline__ void finish(TreeAux<C>* aux, uint8_t* tile_mem, int tile, int context) {
+    if (!values || (tile + 1) * ATTN_UNIT <= context) return;
+    // what is not finite must not meet the zeros of rows that do not see it: left out here, added at the end
+    uint8_t* vd = tile_mem + plane * 8192 + tok * 128 + C::T_BYTES;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      const uint4 x = *reinterpret_cast<uint4*>(vd + i * 16);
+      uint32_t e[4] = {x.x, x.y, x.z, x.w};
+      bool hit = false;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (keys) copy16(ptx::smem_u32(kd + i * 16), p + i * 16, bytes);
-        if (values) copy16(ptx::smem_u32(vd + i * 16), good ? p + C::PLANES * a.plane_bytes + i * 16 : p, bytes);
-      }
-      asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-      if (values && (tile + 1) * ATTN_UNIT > context) {
-        // what is not finite must not meet the zeros of rows that do not see it: left out here, added at the end
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          uint4 x = *reinterpret_cast<uint4*>(vd + i * 16);
-          uint32_t* e = &x.x;
-          bool hit = false;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (not_finite2(e[j])) {
-              hit = true;
-              if ((e[j] & 0x7F80u) == 0x7F80u) e[j] &= 0xFFFF0000u;
-              if ((e[j] & 0x7F800000u) == 0x7F800000u) e[j] &= 0x0000FFFFu;
-            }
-          if (hit) {
-            *reinterpret_cast<uint4*>(vd + i * 16) = x;
-            *reinterpret_cast<volatile int*>(&aux->odd) = 1;
-          }
+      for (int j = 0; j < 4; ++j)
+        if (not_finite2(e[j])) {
+          hit = true;
+          if ((e[j] & 0x7F80u) == 0x7F80u) e[j] &= 0xFFFF0000u;
+          if ((e[j] & 0x7F800000u) == 0x7F800000u) e[j] &= 0x0000FFFFu;
         }
+      if (hit) {
+        *reinterpret_cast<uint4*>(vd + i * 16) = make_uint4(e[0], e[1], e[2], e[3]);
+        *reinterpret_cast<volatile int*>(&aux->odd) = 1;
       }
     }
   }
@@ -211,17 +231,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   constexpr int D = C::D, PL = C::PLANES;
-  uint8_t* sQ = smem;
-  uint8_t* sT = smem + C::Q_BYTES;                             // keys, values; keys, values
-  uint8_t* sP = sT + 4 * C::T_BYTES;
-  TreeAux<C>* aux = reinterpret_cast<TreeAux<C>*>(sP + 2 * C::P_BYTES);
+  uint8_t* sT = smem;                                          // stages of keys, values
+  uint8_t* sRaw = sT + 2 * C::STAGES * C::T_BYTES;
+  TreeAux<C>* aux = reinterpret_cast<TreeAux<C>*>(sRaw + C::RAW * C::RAW_BYTES);
   static_assert(sizeof(TreeAux<C>) <= C::AUX_BYTES, "TreeCfg::AUX_BYTES");
+  constexpr int S = C::STAGES, STAGE = 2 * C::T_BYTES;
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
   volatile int* abort_flag = &aux->abort_flag;
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < S; ++i) {
       ptx::mbar_init(&aux->full[i], 128);
+      ptx::mbar_init(&aux->empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&aux->scored[i], 1);
+      ptx::mbar_init(&aux->read[i], 128);
       ptx::mbar_init(&aux->ready[i], 128);
       ptx::mbar_init(&aux->done[i], 1);
     }
@@ -234,190 +258,266 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
     b.begin(a);
     if (lane == 0) aux->w = b;
   }
-  if (warp == 8) {
-    ptx::tmem_alloc(&aux->tmem, 256);
+  if (warp == 12) {
+    ptx::tmem_alloc(&aux->tmem, 512);
     ptx::tmem_relinquish();
   }
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = aux->tmem, tO = tmem + 128;            // S: two buffers of 64 columns; O: D columns
+  const uint32_t tmem = aux->tmem, tO = tmem + C::T_O, tQ = tmem + C::T_Q, tP = tmem + C::T_P;
   Walk<C> w = aux->w;
-  int cnt = 0;                                                 // tiles so far: buffer cnt & 1, phase (cnt >> 1) & 1
+  int cnt = 0;                                                 // tiles so far: stream and buffers cnt & 1, phase (cnt >> 1) & 1; stage cnt % S
   bool head_of_run = true, more = w.left > 0;
 
   while (more) {
     // ---- the item's rows
-    if (warp < 8) {
-      const int kh = w.item % a.kv_heads, first = (w.item / a.kv_heads) * C::ROWS, rows = w.s.nodes * a.group;
-      for (int i = tid; i < 128 * (D / 8); i += 256) {
-        const int r = i / (D / 8), ch = i % (D / 8);
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (first + r < rows) {
-          const int node = (first + r) / a.group;
-          x = *reinterpret_cast<const uint4*>(a.q + (long long)(w.s.start + node) * a.q_t + (long long)(kh * a.group + first + r - node * a.group) * a.q_h + ch * 8);
+    if (warp < 4) {
+      const TreeRow row = tree_row<C>(a, w.s, w.item, tid);
+      const __nv_bfloat16* q = a.q + row.row * a.q_t + row.head * a.q_h;
+#pragma unroll
+      for (int c = 0; c < D / 2; c += 16) {
+        uint32_t x[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint4 y = row.real ? *reinterpret_cast<const uint4*>(q + 2 * c + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
+          x[4 * j] = y.x; x[4 * j + 1] = y.y; x[4 * j + 2] = y.z; x[4 * j + 3] = y.w;
         }
-        *reinterpret_cast<uint4*>(sQ + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = x;
+        tmem_write16(tQ + ((uint32_t)(warp * 32) << 16) + c, x);
       }
       if (tid == 0) aux->odd = 0;
-      ptx::fence_proxy_async();
+      tmem_write_wait();
+      ptx::tc_fence_before();
     }
     __syncthreads();
+    ptx::tc_fence_after();
     const int tiles = w.end - w.tile;
     const int len = w.s.context + w.s.nodes;
 
-    if (warp >= 4 && warp < 8) {
+    if (warp >= 8 && warp < 12) {
       // ------------------------------------------------------------ keys and values
       Bring<C> in;
-      in.item(a, w, tid - 128);
+      const int id = tid - 256;
+      in.item(a, w, id);
+      in.later = in.look(a, w.tile, w.end);
       in.ask(a, w.tile, w.end);
-      in.load(a, w.tile);
-      in.ask(a, w.tile + 1, w.end);
+      in.goods = 0;
+      if (C::BITS == 4)
+        for (int k = 0; k < C::RAW; ++k) {
+          in.fetch(a, sRaw, k, w.tile + k, id);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          in.ask(a, w.tile + k + 1, w.end);
+        }
+      int st = cnt % S, slot = 0;
+      uint32_t ph = ((uint32_t)(cnt / S) & 1u) ^ 1u;
       for (int i = 0; i < tiles; ++i) {
-        const int n = cnt + i, buf = n & 1;
-        if (!tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag)) break;
-        in.put(a, aux, sT + buf * 2 * C::T_BYTES, buf, w.tile + i, w.s.context);
-        ptx::fence_proxy_async();
-        ptx::mbar_arrive(&aux->full[buf]);
-        in.load(a, w.tile + i + 1);
-        in.ask(a, w.tile + i + 2, w.end);
+        if (!tc_wait_warp(&aux->empty[st], ph, abort_flag)) break;
+        uint8_t* mem = sT + st * STAGE;
+        if (C::BITS == 16) {
+          in.copy(a, mem, w.tile + i);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          in.lost(a, aux, st, w.tile + i, (unsigned)in.cur < (unsigned)a.pages, id);
+          in.ask(a, w.tile + i + 1, w.end);
+          // this tile's copies are issued, those of the one before are there
+          if (i > 0) {
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            const int before = st == 0 ? S - 1 : st - 1;
+            in.finish(aux, sT + before * STAGE, w.tile + i - 1, w.s.context);
+            ptx::fence_proxy_async();
+            ptx::mbar_arrive(&aux->full[before]);
+          }
+          if (i + 1 == tiles) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            in.finish(aux, mem, w.tile + i, w.s.context);
+            ptx::fence_proxy_async();
+            ptx::mbar_arrive(&aux->full[st]);
+          }
+        } else {
+          asm volatile("cp.async.wait_group %0;" ::"n"(C::RAW > 0 ? C::RAW - 1 : 0) : "memory");
+          in.put(a, aux, mem, sRaw, slot, st, id);
+          in.lost(a, aux, st, w.tile + i, (in.goods >> slot) & 1u, id);
+          ptx::fence_proxy_async();
+          ptx::mbar_arrive(&aux->full[st]);
+          in.fetch(a, sRaw, slot, w.tile + i + C::RAW, id);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          in.ask(a, w.tile + i + C::RAW + 1, w.end);
+          slot = slot + 1 == C::RAW ? 0 : slot + 1;
+        }
+        if (++st == S) { st = 0; ph ^= 1u; }
       }
-    } else if (warp == 8) {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+    } else if (warp == 12) {
       // ------------------------------------------------------------ products
       const uint32_t leader = ptx::elect_one();
       const uint32_t base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
       const uint32_t id_s = base | ((uint32_t)(64 >> 3) << 17), id_o = base | (1u << 16) | ((uint32_t)(D >> 3) << 17);
-      const uint32_t q0 = ptx::smem_u32(sQ), t0 = ptx::smem_u32(sT), p0 = ptx::smem_u32(sP);
+      const uint32_t t0 = ptx::smem_u32(sT);
       auto scores = [&](int n) {
-        const int buf = n & 1;
-        if (!tc_wait_warp(&aux->full[buf], (n >> 1) & 1, abort_flag)) return false;
+        const int st = n % S;
+        if (!tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag)) return false;
         ptx::tc_fence_after();
-        const uint32_t k0 = t0 + buf * 2 * C::T_BYTES;
+        const uint32_t k0 = t0 + st * STAGE;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
-          ptx::umma_bf16_by<false>(leader, tmem + buf * 64, tc_smem_desc(q0 + (j >> 2) * 16384 + (j & 3) * 32, 16, 1024),
-                                   tc_smem_desc(k0 + (j >> 2) * 8192 + (j & 3) * 32, 16, 1024), id_s, j > 0 ? 1u : 0u);
-        ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->scored[buf]));
+          umma_from_tmem(leader, tmem + (n & 1) * 64, tQ + j * 8, tc_smem_desc(k0 + (j >> 2) * 8192 + (j & 3) * 32, 16, 1024), id_s, j > 0 ? 1u : 0u);
+        ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->scored[n & 1]));
         return true;
       };
-      bool ok = scores(cnt);
+      bool ok = scores(cnt) && (tiles < 2 || scores(cnt + 1));
       for (int i = 0; ok && i < tiles; ++i) {
         const int n = cnt + i, buf = n & 1;
-        // the buffer of the next scores was read before P of the tile before this one was written
-        if (i + 1 < tiles && !(ok = scores(n + 1))) break;
+        if (i + 2 < tiles) {
+          if (!(ok = tc_wait_warp(&aux->read[buf], (n >> 1) & 1, abort_flag))) break;
+          ptx::tc_fence_after();
+          if (!(ok = scores(n + 2))) break;
+        }
         if (!(ok = tc_wait_warp(&aux->ready[buf], (n >> 1) & 1, abort_flag))) break;
         ptx::tc_fence_after();
-        const uint32_t v0 = t0 + buf * 2 * C::T_BYTES + C::T_BYTES;
+        const uint32_t v0 = t0 + (n % S) * STAGE + C::T_BYTES;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          ptx::umma_bf16_by<false>(leader, tO, tc_smem_desc(p0 + buf * C::P_BYTES + j * 32, 16, 1024), tc_smem_desc(v0 + j * 2048, 8192, 1024), id_o,
-                                   (i > 0 || j > 0) ? 1u : 0u);
+          umma_from_tmem(leader, tO + buf * 128, tP + buf * 32 + j * 8, tc_smem_desc(v0 + j * 2048, 8192, 1024), id_o, (i > 1 || j > 0) ? 1u : 0u);
         ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->done[buf]));
+        ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->empty[n % S]));
       }
     } else {
-      // ------------------------------------------------------------ a row a thread
-      const TreeRow row = tree_row<C>(a, w.s, w.item, tid);
-      const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+      // ------------------------------------------------------------ a row a thread, every other tile
+      const int buf = warp >> 2, r = tid & 127;
+      const TreeRow row = tree_row<C>(a, w.s, w.item, r);
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       float m = -INFINITY, l = 0.f;
       bool ok = true;
-      for (int i = 0; i < tiles; ++i) {
-        const int n = cnt + i, buf = n & 1, first = (w.tile + i) * ATTN_UNIT;
-        // (the steps come with the tile, the scores with its product)
-        if (!(ok = tc_wait_warp(&aux->full[buf], (n >> 1) & 1, abort_flag) && tc_wait_warp(&aux->scored[buf], (n >> 1) & 1, abort_flag))) break;
+      const int i0 = (cnt ^ buf) & 1;                          // the stream's first tile of this item
+      for (int i = i0; i < tiles; i += 2) {
+        const int n = cnt + i, st = n % S, first = (w.tile + i) * ATTN_UNIT;
+        // (the steps come with the tile, the scores with its product; P and O of the stream's tile before)
+        if (!(ok = tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag) && tc_wait_warp(&aux->scored[buf], (n >> 1) & 1, abort_flag) &&
+                   tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag)))
+          break;
         ptx::tc_fence_after();
-        float s[2][32];
-        ptx::tmem_ld32(tmem + lanes + buf * 64, s[0]);
-        ptx::tmem_ld32(tmem + lanes + buf * 64 + 32, s[1]);
-        const unsigned long long bad = (unsigned long long)aux->bad[buf][0] | ((unsigned long long)aux->bad[buf][1] << 32);
+        const uint32_t tS = tmem + lanes + buf * 64;
+        const unsigned long long bad = (unsigned long long)aux->bad[st][0] | ((unsigned long long)aux->bad[st][1] << 32);
         const bool edge = first + ATTN_UNIT > w.s.context || bad != 0ull;
         const unsigned long long see = edge ? seen64(row.mask, w.s.context, first) & ~bad : ~0ull;
-        float top = -INFINITY;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
+        auto kstep = [&](int j) { return C::BITS == 4 ? *reinterpret_cast<const float4*>(&aux->kstep[st][j]) : make_float4(a.scale, a.scale, a.scale, a.scale); };
+        float sum0 = 0.f, sum1 = 0.f;                          // a tile's probabilities by themselves: fewer roundings of a long sum
+        // 32 columns at a time; where a score exceeds the bound (none yet: any does) the bound is raised and the tile begins again
+        for (int h = 0; h < 2; ++h) {
+          float s[32];
+          ptx::tmem_ld32(tS + h * 32, s);
+          const float neg = m == -INFINITY ? INFINITY : -m;
+          float top = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
-            float4 k = make_float4(a.scale, a.scale, a.scale, a.scale);
-            if (C::BITS == 4) k = *reinterpret_cast<const float4*>(&aux->kstep[buf][h * 32 + j]);
-            s[h][j] *= k.x; s[h][j + 1] *= k.y; s[h][j + 2] *= k.z; s[h][j + 3] *= k.w;
+            const float4 k = kstep(h * 32 + j);
+            s[j] = fmaf(s[j], k.x, neg); s[j + 1] = fmaf(s[j + 1], k.y, neg); s[j + 2] = fmaf(s[j + 2], k.z, neg); s[j + 3] = fmaf(s[j + 3], k.w, neg);
           }
-        if (edge) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
+          if (edge) {
+            const uint32_t bits = (uint32_t)(see >> (h * 32));
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (!((see >> (h * 32 + j)) & 1ull)) s[h][j] = -INFINITY;
-        }
+              if (!((bits >> j) & 1u)) s[j] = -INFINITY;
+          }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < 32; ++j) top = fmaxf(top, s[h][j]);
-        const bool up = top > m + 8.f;                         // (no bound yet: m = -inf, and any score exceeds it)
-        if (__any_sync(0xffffffffu, up)) {
-          const float f = up ? ex2(m - top) : 1.f;
-          if (up) m = top;
-          l *= f;
-          if (i > 0) {                                         // (the first tile's product overwrites O)
-            if (!(ok = tc_wait_warp(&aux->done[(n - 1) & 1], ((n - 1) >> 1) & 1, abort_flag))) break;
-            ptx::tc_fence_after();
+          for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(s[j], s[j + 1]));
+          if (__any_sync(0xffffffffu, top > 8.f)) {
+            top = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {
-              uint32_t o[16];
-              tmem_read16(tO + lanes + c, o);
+            for (int g = 0; g < 2; ++g) {
+              ptx::tmem_ld32(tS + g * 32, s);
+              const uint32_t bits = (uint32_t)(see >> (g * 32));
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_write16(tO + lanes + c, o);
+              for (int j = 0; j < 32; j += 4) {
+                const float4 k = kstep(g * 32 + j);
+                if (bits & (1u << j)) top = fmaxf(top, s[j] * k.x);
+                if (bits & (2u << j)) top = fmaxf(top, s[j + 1] * k.y);
+                if (bits & (4u << j)) top = fmaxf(top, s[j + 2] * k.z);
+                if (bits & (8u << j)) top = fmaxf(top, s[j + 3] * k.w);
+              }
             }
-            tmem_write_wait();
+            const bool up = top > m;                           // (rows below theirs are raised too: no harm)
+            const float f = up ? ex2(m - top) : 1.f;
+            if (up) m = top;
+            l *= f;
+            if (i > i0) {                                      // (the item's first tile overwrites O)
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                uint32_t o[16];
+                tmem_read16(tO + buf * 128 + lanes + c, o);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                tmem_write16(tO + buf * 128 + lanes + c, o);
+              }
+              tmem_write_wait();
+            }
+            sum0 = sum1 = 0.f;
+            h = -1;
+            continue;
           }
-        }
-        const float bound = m == -INFINITY ? 0.f : m;
-        // P of two tiles ago has been read when its product is complete
-        if (!(ok = tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag))) break;
-        uint8_t* prow = sP + buf * C::P_BYTES + tid * 128;
-        float sum = 0.f;                                       // a tile's probabilities by themselves: fewer roundings of a long sum
+          if (h == 1) {
+            ptx::tc_fence_before();
+            ptx::mbar_arrive(&aux->read[buf]);
+          }
+          uint32_t p[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < 32; j += 8) {
-            float p[8];
-            float4 v0 = make_float4(1.f, 1.f, 1.f, 1.f), v1 = v0;
+          for (int j = 0; j < 32; j += 4) {
+            float e0 = ex2(s[j]), e1 = ex2(s[j + 1]), e2 = ex2(s[j + 2]), e3 = ex2(s[j + 3]);
+            sum0 += e0 + e2;
+            sum1 += e1 + e3;
             if (C::BITS == 4) {
-              v0 = *reinterpret_cast<const float4*>(&aux->vstep[buf][h * 32 + j]);
-              v1 = *reinterpret_cast<const float4*>(&aux->vstep[buf][h * 32 + j + 4]);
+              const float4 v = *reinterpret_cast<const float4*>(&aux->vstep[st][h * 32 + j]);
+              e0 *= v.x; e1 *= v.y; e2 *= v.z; e3 *= v.w;
+              if (edge) {                                      // an unseen record may say NaN
+                if (s[j] == -INFINITY) e0 = 0.f;
+                if (s[j + 1] == -INFINITY) e1 = 0.f;
+                if (s[j + 2] == -INFINITY) e2 = 0.f;
+                if (s[j + 3] == -INFINITY) e3 = 0.f;
+              }
             }
-            const float vs[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float q = ex2(s[h][j + e] - bound);
-              sum += q;
-              p[e] = C::BITS == 4 ? q * vs[e] : q;
-              if (C::BITS == 4 && edge && s[h][j + e] == -INFINITY) p[e] = 0.f;      // an unseen record may say NaN
-            }
-            *reinterpret_cast<uint4*>(prow + (((h * 4 + j / 8) ^ (tid & 7)) << 4)) =
-                make_uint4(bf16x2(p[0], p[1]), bf16x2(p[2], p[3]), bf16x2(p[4], p[5]), bf16x2(p[6], p[7]));
+            p[j / 2] = bf16x2(e0, e1);
+            p[j / 2 + 1] = bf16x2(e2, e3);
           }
-        l += sum;
-        ptx::fence_proxy_async();
+          tmem_write16(tP + lanes + buf * 32 + h * 16, p);
+        }
+        l += sum0 + sum1;
+        tmem_write_wait();
         ptx::tc_fence_before();
         ptx::mbar_arrive(&aux->ready[buf]);
       }
-      const int last = cnt + tiles - 1;
-      if (ok) ok = tc_wait_warp(&aux->done[last & 1], (last >> 1) & 1, abort_flag);
+      const int mine = tiles > i0 ? (tiles - 1 - i0) / 2 : -1, last = cnt + i0 + 2 * mine;      // the stream's last tile of the item
+      if (ok && mine >= 0) ok = tc_wait_warp(&aux->done[buf], (last >> 1) & 1, abort_flag);
       ptx::tc_fence_after();
-      bar_sync(BAR_ALL, 128);
+      aux->bound[buf][r] = m;
+      aux->sum[buf][r] = l;
+      bar_sync(BAR_ALL, 256);
       if (!*abort_flag) {
         const bool whole = w.tile == 0 && w.end == w.s.tiles;
+        // the two streams together; each group of warps takes half of the columns
+        const float m0 = aux->bound[0][r], m1 = aux->bound[1][r];
+        m = m1 > m0 ? m1 : m0;
+        const bool two = tiles > 1;
+        float f[2] = {m == -INFINITY ? 1.f : ex2(m0 - m), m == -INFINITY ? 1.f : ex2(m1 - m)};
+        l = aux->sum[0][r] * f[0] + aux->sum[1][r] * f[1];
         const bool none = l == 0.f && m == -INFINITY;
-        float* part = a.parts + (2 * (size_t)blockIdx.x + (head_of_run ? 0 : 1)) * C::SLOT + tid;
-        const float inv = none ? 0.f : 1.f / l;
+        float* part = a.parts + (2 * (size_t)blockIdx.x + (head_of_run ? 0 : 1)) * C::SLOT + r;
+        if (whole) {
+          const float inv = none ? 0.f : 1.f / l;
+          f[0] *= inv;
+          f[1] *= inv;
+        }
+        const int only = (cnt & 1);                            // the stream of the item's first tile
         const int odd = C::BITS == 16 ? *reinterpret_cast<volatile int*>(&aux->odd) : 0;
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
+        for (int c = buf * (D / 2); c < (buf + 1) * (D / 2); c += 32) {
           float o[32];
-          ptx::tmem_ld32(tO + lanes + c, o);
-          if (whole) {
+          ptx::tmem_ld32(tO + only * 128 + lanes + c, o);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] *= inv;
+          for (int j = 0; j < 32; ++j) o[j] *= f[only];
+          if (two) {
+            float x[32];
+            ptx::tmem_ld32(tO + (only ^ 1) * 128 + lanes + c, x);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = fmaf(x[j], f[only ^ 1], o[j]);
           }
           if (C::BITS == 16 && odd && row.real) {
             // values that are not finite, of the tokens that the row sees (rare)
@@ -447,50 +547,56 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
           }
         }
         if (whole) {
-          if (row.real && a.lse) a.lse[row.row * a.lse_t + row.head] = none ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
+          if (buf == 0 && row.real && a.lse) a.lse[row.row * a.lse_t + row.head] = none ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
         } else {
-          __stcg(part + D * 128, m);
-          __stcg(part + (D + 1) * 128, l);
+          if (buf == 0) {
+            __stcg(part + D * 128, m);
+            __stcg(part + (D + 1) * 128, l);
+          }
           __threadfence();
-          bar_sync(BAR_ALL, 128);
+          bar_sync(BAR_ALL, 256);
           const int c0 = w.owner(w.item_at), c1 = w.owner(w.item_at + w.s.tiles - 1);
           if (tid == 0) {
             const unsigned n = (unsigned)(c1 - c0);
             aux->last = atomicInc(a.counters + c0, n) == n;
             __threadfence();
           }
-          bar_sync(BAR_ALL, 128);
+          bar_sync(BAR_ALL, 256);
           if (aux->last) {
-            auto slot = [&](int k) { return a.parts + (2 * (size_t)k + (w.run_begin(k) < w.item_at ? 1 : 0)) * C::SLOT + tid; };
+            auto slot = [&](int k) { return a.parts + (2 * (size_t)k + (w.run_begin(k) < w.item_at ? 1 : 0)) * C::SLOT + r; };
+            // the parts' loads go out several at a time: their latency is what this costs
             float tm = -INFINITY, tl = 0.f;
-            for (int k = c0; k <= c1; ++k) {
-              const float* p = slot(k);
-              const float om = __ldcg(p + D * 128), ol = __ldcg(p + (D + 1) * 128);
-              const float to = om > tm ? om : tm;
-              tl = tl * (to == -INFINITY ? 1.f : ex2(tm - to)) + ol * (to == -INFINITY ? 1.f : ex2(om - to));
-              tm = to;
+            for (int k = c0; k <= c1; k += 8) {
+              float om[8], ol[8];
+#pragma unroll
+              for (int u = 0; u < 8; ++u) {
+                const float* p = slot(min(k + u, c1));
+                om[u] = k + u <= c1 ? __ldcg(p + D * 128) : -INFINITY;
+                ol[u] = k + u <= c1 ? __ldcg(p + (D + 1) * 128) : 0.f;
+              }
+#pragma unroll
+              for (int u = 0; u < 8; ++u) {
+                const float to = om[u] > tm ? om[u] : tm;
+                tl = tl * (to == -INFINITY ? 1.f : ex2(tm - to)) + ol[u] * (to == -INFINITY ? 1.f : ex2(om[u] - to));
+                tm = to;
+              }
             }
             const bool zero = tl == 0.f && tm == -INFINITY;
             const float ti = zero ? 0.f : 1.f / tl;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              float o[32];
-#pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = 0.f;
+            for (int c = buf * (D / 2); c < (buf + 1) * (D / 2); c += 8) {
+              float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
               for (int k = c0; k <= c1; ++k) {
                 const float* p = slot(k);
                 const float om = __ldcg(p + D * 128), f = (tm == -INFINITY ? 1.f : ex2(om - tm)) * ti;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) o[j] = fmaf(__ldcg(p + (c + j) * 128), f, o[j]);
+                for (int j = 0; j < 8; ++j) o[j] = fmaf(__ldcg(p + (c + j) * 128), f, o[j]);
               }
-              if (row.real) {
-                __nv_bfloat16* out = a.out + row.row * a.o_t + row.head * a.o_h + c;
-#pragma unroll
-                for (int j = 0; j < 32; j += 8)
-                  *reinterpret_cast<uint4*>(out + j) = make_uint4(bf16x2(o[j], o[j + 1]), bf16x2(o[j + 2], o[j + 3]), bf16x2(o[j + 4], o[j + 5]), bf16x2(o[j + 6], o[j + 7]));
-              }
+              if (row.real)
+                *reinterpret_cast<uint4*>(a.out + row.row * a.o_t + row.head * a.o_h + c) = make_uint4(bf16x2(o[0], o[1]), bf16x2(o[2], o[3]), bf16x2(o[4], o[5]), bf16x2(o[6], o[7]));
             }
-            if (row.real && a.lse) a.lse[row.row * a.lse_t + row.head] = zero ? -INFINITY : (tm == -INFINITY ? 0.f : tm) * 0.6931471805599453f + logf(tl);
+            if (buf == 0 && row.real && a.lse) a.lse[row.row * a.lse_t + row.head] = zero ? -INFINITY : (tm == -INFINITY ? 0.f : tm) * 0.6931471805599453f + logf(tl);
           }
         }
       }
@@ -506,7 +612,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
   if (tid == 0 && *abort_flag) atomicOr(a.flags, KV_FLAG_TIMEOUT);
   ptx::tc_fence_before();
   __syncthreads();
-  if (warp == 8) ptx::tmem_dealloc(tmem, 256);
+  if (warp == 12) ptx::tmem_dealloc(tmem, 512);
 }
 
 }  // namespace kv
