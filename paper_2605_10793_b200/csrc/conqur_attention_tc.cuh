@@ -19,11 +19,11 @@ namespace kv {
 template <int BITS_, int D_>
 struct TreeCfg {
   static constexpr int BITS = BITS_, D = D_;
-  static constexpr int ROWS = 128, THREADS = 416, PLANES = D / 64, STAGES = 4;
+  static constexpr int ROWS = 128, THREADS = 640, PLANES = D / 64, STAGES = 4;
   static constexpr int T_BYTES = PLANES * 8192;                // keys or values of a tile
-  static constexpr int RAW = BITS == 4 ? 4 : 0, RAW_BYTES = 9216;   // tiles of codes on their way: 64 bytes and two records a thread
+  static constexpr int RAW = 2, RAW_BYTES = 9728;   // tiles of codes on their way: 64 bytes and two records a thread; page numbers
   static constexpr int AUX_BYTES = 5120;
-  static constexpr int SMEM = 1024 + 2 * STAGES * T_BYTES + RAW * RAW_BYTES + AUX_BYTES;
+  static constexpr int SMEM = 1024 + 2 * STAGES * T_BYTES + (BITS == 4 ? 2 * RAW * RAW_BYTES : 0) + AUX_BYTES;
   // TMEM columns: scores 2 x 64, accumulators 2 x 128, the rows D / 2 (two bf16 a column), probabilities 2 x 32
   static constexpr int T_O = 128, T_Q = 384, T_P = 448;
   static_assert(SMEM <= 227 * 1024, "shared memory of an SM");
@@ -58,6 +58,21 @@ __device__ __forceinline__ void tmem_write16(uint32_t taddr, const uint32_t (&w)
         "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
       : "memory");
 }
+// 64 columns with one wait.
+__device__ __forceinline__ void tmem_read64(uint32_t taddr, float (&v)[64]) {
+  uint32_t r[4][16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[i][0]), "=r"(r[i][1]), "=r"(r[i][2]), "=r"(r[i][3]), "=r"(r[i][4]), "=r"(r[i][5]), "=r"(r[i][6]), "=r"(r[i][7]), "=r"(r[i][8]),
+          "=r"(r[i][9]), "=r"(r[i][10]), "=r"(r[i][11]), "=r"(r[i][12]), "=r"(r[i][13]), "=r"(r[i][14]), "=r"(r[i][15])
+        : "r"(taddr + 16 * i)
+        : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i >> 4][i & 15]);
+}
 // D(tmem) (+)= A(tmem: lane = row, two consecutive k a column) B(smem)
 __device__ __forceinline__ void umma_from_tmem(uint32_t leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -66,6 +81,18 @@ __device__ __forceinline__ void umma_from_tmem(uint32_t leader, uint32_t tmem_d,
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(leader)
       : "memory");
+}
+// One look at a barrier, without the hardware's suspension of a waiting thread; the whole warp agrees.
+__device__ __forceinline__ bool arrived(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(ptx::smem_u32(bar)), "r"(parity)
+      : "memory");
+  return __all_sync(0xffffffffu, ok != 0u);
 }
 __device__ __forceinline__ void tmem_write_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -91,8 +118,10 @@ struct Bring {
   const int* table;
   const uint8_t* head;
   int len;
-  int page, later, cur;              // of the next tile to fetch and of the one after (asked for two ahead); 16 bits: of the one being brought
-  uint32_t goods;                    // a bit a slot of the ring: the page could be read
+  int page;                          // 4 bits: of the next tile to fetch
+  int now[2], next[2];               // 16 bits: of tokens lane and lane + 32 of the tile being brought and of the group's next
+  uint32_t goods, ahead;             // a bit a slot of the ring: the page could be read; a page number comes with it
+  int last;                          // end of the item's tiles in this run
 
   __device__ __forceinline__ void item(const AttnArgs& a, const Walk<C>& w, int tid) {
     tok = tid & 63;
@@ -103,17 +132,17 @@ struct Bring {
     table = a.table + (long long)w.b * a.table_stride;
     head = a.cache + (long long)(w.item % a.kv_heads) * a.block_bytes;
     len = w.s.context + w.s.nodes;
+    last = w.end;
+    goods = ahead = 0u;
   }
-  __device__ __forceinline__ int look(const AttnArgs& a, int tile, int end) const {
-    const int pos = tile * ATTN_UNIT + tok;
-    return tile < end && pos < len && (pos >> a.log_page) < a.table_width ? table[pos >> a.log_page] : -1;
+  __device__ __forceinline__ int look(const AttnArgs& a, int tile, int at) const {
+    const int pos = tile * ATTN_UNIT + at;
+    return tile < last && pos < len && (pos >> a.log_page) < a.table_width ? table[pos >> a.log_page] : -1;
   }
-  // The page of `tile` moves up, that of the one after is asked for.
-  __device__ __forceinline__ void ask(const AttnArgs& a, int tile, int end) {
-    page = later;
-    later = look(a, tile + 1, end);
+  __device__ __forceinline__ void ask(const AttnArgs& a, int tile, int lane) {
+    next[0] = look(a, tile, lane);
+    next[1] = look(a, tile, lane + 32);
   }
-  __device__ __forceinline__ const uint8_t* block(const AttnArgs& a) const { return head + (long long)cur * a.page_bytes; }
   // 4 bits: the codes of the tile whose page was asked for, into this thread's places of a slot (zeros where there is no page)
   __device__ __forceinline__ void fetch(const AttnArgs& a, uint8_t* raw, int slot, int tile, int tid) {
     const bool good = (unsigned)page < (unsigned)a.pages;
@@ -130,6 +159,11 @@ struct Bring {
       copy16(to + 4096, c + a.codes_bytes, n);
       copy16(to + 6144, c + a.codes_bytes + 16, n);
     }
+    // the page number of the tile that takes this slot next comes along
+    const int next = tile + 2 * C::RAW, npos = next * ATTN_UNIT + tok;
+    const bool have = next < last && npos < len && (npos >> a.log_page) < a.table_width;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(ptx::smem_u32(raw + slot * C::RAW_BYTES) + 9216 + tid * 4), "l"(have ? table + (npos >> a.log_page) : a.starts), "r"(have ? 4 : 0) : "memory");
+    ahead = (ahead & ~(1u << slot)) | ((have ? 1u : 0u) << slot);
     const uint32_t rec = ptx::smem_u32(raw + slot * C::RAW_BYTES) + 8192 + tid * 8;
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(rec), "l"(p + 2 * a.codes_bytes + at * 4), "r"(n / 4) : "memory");
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(rec + 4), "l"(p + 2 * a.codes_bytes + (a.page_size + at) * 4), "r"(n / 4) : "memory");
@@ -139,10 +173,11 @@ struct Bring {
 #pragma unroll
     for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(row + ((i ^ (t & 7)) << 4)) = codes8(w[i], bias);
   }
-  __device__ __forceinline__ void lost(const AttnArgs& a, TreeAux<C>* aux, int st, int tile, bool good, int tid) {
-    const unsigned x = __ballot_sync(0xffffffffu, !good && tile * ATTN_UNIT + tok < len);
-    if (tid < 64 && (tid & 31) == 0) {
-      aux->bad[st][tid >> 5] = x;
+  // Tokens of the tile whose page cannot be read, 32 a warp.
+  __device__ __forceinline__ void lost(const AttnArgs& a, TreeAux<C>* aux, int st, int tile, bool good, int half, int at) {
+    const unsigned x = __ballot_sync(0xffffffffu, !good && tile * ATTN_UNIT + at < len);
+    if ((at & 31) == 0) {
+      aux->bad[st][half] = x;
       if (x) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
     }
   }
@@ -157,27 +192,28 @@ struct Bring {
     if (tid < 64) aux->kstep[st][tok] = step_of(rec.x) * a.scale;                // the scale has the 64 of the codes
     else aux->vstep[st][tok] = step_of(rec.y) * 64.f;
   }
-  // 16 bits: the copies of the next tile (one group), and what is left to do when they are there
-  __device__ __forceinline__ void copy(const AttnArgs& a, uint8_t* tile_mem, int tile) {
-    cur = page;
-    const bool good = (unsigned)cur < (unsigned)a.pages;
-    uint8_t* kd = tile_mem + plane * 8192 + tok * 128;
-    uint8_t* vd = kd + C::T_BYTES;
-    const int at = (tile * ATTN_UNIT + tok) & (a.page_size - 1), bytes = good ? 16 : 0;
-    const uint8_t* p = good ? block(a) + plane * a.plane_bytes + at * 128 : a.cache;
+  // 16 bits: the copies of a tile (one group of copies): eight threads a row of 128 bytes, sixteen rows at a time
+  __device__ __forceinline__ void copy(const AttnArgs& a, uint8_t* tile_mem, int tile, int tid) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (keys) copy16(ptx::smem_u32(kd + i * 16), p + i * 16, bytes);
-      if (values) copy16(ptx::smem_u32(vd + i * 16), good ? p + C::PLANES * a.plane_bytes + i * 16 : p, bytes);
+    for (int k = 0; k < 4; ++k) {
+      const int row = 16 * k + (tid >> 3), page = __shfl_sync(0xffffffffu, now[k >> 1], row & 31);
+      const bool good = (unsigned)page < (unsigned)a.pages;
+      const int bytes = good ? 16 : 0;
+      const uint8_t* p = good ? head + (long long)page * a.page_bytes + ((tile * ATTN_UNIT + row) & (a.page_size - 1)) * 128 + (tid & 7) * 16 : a.cache;
+      const long long step = good ? a.plane_bytes : 0;
+      const uint32_t to = ptx::smem_u32(tile_mem) + row * 128 + (tid & 7) * 16;
+#pragma unroll
+      for (int i = 0; i < 2 * C::PLANES; ++i) copy16(to + i * 8192, p + i * step, bytes);
     }
   }
-  __device__ __forceinline__ void finish(TreeAux<C>* aux, uint8_t* tile_mem, int tile, int context) {
-    if (!values || (tile + 1) * ATTN_UNIT <= context) return;
-    // what is not finite must not meet the zeros of rows that do not see it: left out here, added at the end
-    uint8_t* vd = tile_mem + plane * 8192 + tok * 128 + C::T_BYTES;
+  // What is left to do when this thread's copies are there: values that are not finite must not meet the zeros of rows that do not see them.  They are
+  // left out here and added at the end.
+  __device__ __forceinline__ void finish(TreeAux<C>* aux, uint8_t* tile_mem, int tile, int context, int tid) {
+    if ((tile + 1) * ATTN_UNIT <= context) return;
 #pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      const uint4 x = *reinterpret_cast<uint4*>(vd + i * 16);
+    for (int i = 0; i < 4 * C::PLANES; ++i) {
+      uint8_t* v = tile_mem + C::T_BYTES + i * 2048 + tid * 16;
+      const uint4 x = *reinterpret_cast<uint4*>(v);
       uint32_t e[4] = {x.x, x.y, x.z, x.w};
       bool hit = false;
 #pragma unroll
@@ -188,7 +224,7 @@ struct Bring {
           if ((e[j] & 0x7F800000u) == 0x7F800000u) e[j] &= 0x0000FFFFu;
         }
       if (hit) {
-        *reinterpret_cast<uint4*>(vd + i * 16) = make_uint4(e[0], e[1], e[2], e[3]);
+        *reinterpret_cast<uint4*>(v) = make_uint4(e[0], e[1], e[2], e[3]);
         *reinterpret_cast<volatile int*>(&aux->odd) = 1;
       }
     }
@@ -226,45 +262,13 @@ __device__ __forceinline__ unsigned long long seen64(unsigned long long mask, in
   return -n < 64 ? mask >> -n : 0ull;
 }
 
-template <typename C>
-__global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs a) {
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  constexpr int D = C::D, PL = C::PLANES;
-  uint8_t* sT = smem;                                          // stages of keys, values
-  uint8_t* sRaw = sT + 2 * C::STAGES * C::T_BYTES;
-  TreeAux<C>* aux = reinterpret_cast<TreeAux<C>*>(sRaw + C::RAW * C::RAW_BYTES);
-  static_assert(sizeof(TreeAux<C>) <= C::AUX_BYTES, "TreeCfg::AUX_BYTES");
-  constexpr int S = C::STAGES, STAGE = 2 * C::T_BYTES;
-  const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
+// One of the three roles' warps through all items of the CTA.
+enum TreeRole { TREE_ROWS, TREE_BRING, TREE_PRODUCTS };
+template <typename C, TreeRole ROLE>
+__device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, uint8_t* sT, uint8_t* sRaw, int warp) {
+  constexpr int D = C::D, PL = C::PLANES, S = C::STAGES, STAGE = 2 * C::T_BYTES;
+  const int tid = threadIdx.x;
   volatile int* abort_flag = &aux->abort_flag;
-  if (tid == 0) {
-    for (int i = 0; i < S; ++i) {
-      ptx::mbar_init(&aux->full[i], 128);
-      ptx::mbar_init(&aux->empty[i], 1);
-    }
-    for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(&aux->scored[i], 1);
-      ptx::mbar_init(&aux->read[i], 128);
-      ptx::mbar_init(&aux->ready[i], 128);
-      ptx::mbar_init(&aux->done[i], 1);
-    }
-    aux->abort_flag = 0;
-    ptx::fence_barrier_init();
-    ptx::fence_proxy_async();
-  }
-  if (warp == 0) {
-    Walk<C> b;
-    b.begin(a);
-    if (lane == 0) aux->w = b;
-  }
-  if (warp == 12) {
-    ptx::tmem_alloc(&aux->tmem, 512);
-    ptx::tmem_relinquish();
-  }
-  ptx::tc_fence_before();
-  __syncthreads();
-  ptx::tc_fence_after();
   const uint32_t tmem = aux->tmem, tO = tmem + C::T_O, tQ = tmem + C::T_Q, tP = tmem + C::T_P;
   Walk<C> w = aux->w;
   int cnt = 0;                                                 // tiles so far: stream and buffers cnt & 1, phase (cnt >> 1) & 1; stage cnt % S
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
 
   while (more) {
     // ---- the item's rows
-    if (warp < 4) {
+    if (ROLE == TREE_ROWS && warp < 4) {
       const TreeRow row = tree_row<C>(a, w.s, w.item, tid);
       const __nv_bfloat16* q = a.q + row.row * a.q_t + row.head * a.q_h;
 #pragma unroll
@@ -294,59 +298,68 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
     const int tiles = w.end - w.tile;
     const int len = w.s.context + w.s.nodes;
 
-    if (warp >= 8 && warp < 12) {
+    if constexpr (ROLE == TREE_BRING) {
       // ------------------------------------------------------------ keys and values
+      // two groups of warps take the tiles of even and odd number
       Bring<C> in;
-      const int id = tid - 256;
+      const int id = tid & 127, group = (warp >> 2) & 1, i0 = (cnt ^ group) & 1;
+      uint8_t* raw = sRaw + group * C::RAW * C::RAW_BYTES;
       in.item(a, w, id);
-      in.later = in.look(a, w.tile, w.end);
-      in.ask(a, w.tile, w.end);
-      in.goods = 0;
-      if (C::BITS == 4)
+      if (C::BITS == 4) {
+        int pages[C::RAW];
+#pragma unroll
+        for (int k = 0; k < C::RAW; ++k) pages[k] = in.look(a, w.tile + i0 + 2 * k, in.tok);
+#pragma unroll
         for (int k = 0; k < C::RAW; ++k) {
-          in.fetch(a, sRaw, k, w.tile + k, id);
+          in.page = pages[k];
+          in.fetch(a, raw, k, w.tile + i0 + 2 * k, id);
           asm volatile("cp.async.commit_group;" ::: "memory");
-          in.ask(a, w.tile + k + 1, w.end);
         }
-      int st = cnt % S, slot = 0;
-      uint32_t ph = ((uint32_t)(cnt / S) & 1u) ^ 1u;
-      for (int i = 0; i < tiles; ++i) {
-        if (!tc_wait_warp(&aux->empty[st], ph, abort_flag)) break;
+      } else {
+        in.ask(a, w.tile + i0, id & 31);
+      }
+      int slot = 0;
+      for (int i = i0; i < tiles; i += 2) {
+        const int n = cnt + i, st = n % S;
+        if (!tc_wait_warp(&aux->empty[st], ((uint32_t)(n / S) & 1u) ^ 1u, abort_flag)) break;
         uint8_t* mem = sT + st * STAGE;
         if (C::BITS == 16) {
-          in.copy(a, mem, w.tile + i);
+          in.now[0] = in.next[0];
+          in.now[1] = in.next[1];
+          in.ask(a, w.tile + i + 2, id & 31);
+          in.copy(a, mem, w.tile + i, id);
           asm volatile("cp.async.commit_group;" ::: "memory");
-          in.lost(a, aux, st, w.tile + i, (unsigned)in.cur < (unsigned)a.pages, id);
-          in.ask(a, w.tile + i + 1, w.end);
-          // this tile's copies are issued, those of the one before are there
-          if (i > 0) {
+          if (id < 64) in.lost(a, aux, st, w.tile + i, (unsigned)(id < 32 ? in.now[0] : in.now[1]) < (unsigned)a.pages, id >> 5, id);
+          // this tile's copies are issued, those of the group's tile before are there; at the end of the item all
+          auto there = [&](int k) {
+            const int at = (cnt + k) % S;
+            in.finish(aux, sT + at * STAGE, w.tile + k, w.s.context, id);
+            ptx::fence_proxy_async();
+            ptx::mbar_arrive(&aux->full[at]);
+          };
+          if (i > i0) {
             asm volatile("cp.async.wait_group 1;" ::: "memory");
-            const int before = st == 0 ? S - 1 : st - 1;
-            in.finish(aux, sT + before * STAGE, w.tile + i - 1, w.s.context);
-            ptx::fence_proxy_async();
-            ptx::mbar_arrive(&aux->full[before]);
+            there(i - 2);
           }
-          if (i + 1 == tiles) {
+          if (i + 2 >= tiles) {
             asm volatile("cp.async.wait_group 0;" ::: "memory");
-            in.finish(aux, mem, w.tile + i, w.s.context);
-            ptx::fence_proxy_async();
-            ptx::mbar_arrive(&aux->full[st]);
+            there(i);
           }
         } else {
-          asm volatile("cp.async.wait_group %0;" ::"n"(C::RAW > 0 ? C::RAW - 1 : 0) : "memory");
-          in.put(a, aux, mem, sRaw, slot, st, id);
-          in.lost(a, aux, st, w.tile + i, (in.goods >> slot) & 1u, id);
+          asm volatile("cp.async.wait_group %0;" ::"n"(C::RAW - 1) : "memory");
+          in.put(a, aux, mem, raw, slot, st, id);
+          if (id < 64) in.lost(a, aux, st, w.tile + i, (in.goods >> slot) & 1u, id >> 5, id);
           ptx::fence_proxy_async();
           ptx::mbar_arrive(&aux->full[st]);
-          in.fetch(a, sRaw, slot, w.tile + i + C::RAW, id);
+          in.page = (in.ahead >> slot) & 1u ? *reinterpret_cast<const int*>(raw + slot * C::RAW_BYTES + 9216 + id * 4) : -1;
+          in.fetch(a, raw, slot, w.tile + i + 2 * C::RAW, id);
           asm volatile("cp.async.commit_group;" ::: "memory");
-          in.ask(a, w.tile + i + C::RAW + 1, w.end);
           slot = slot + 1 == C::RAW ? 0 : slot + 1;
         }
-        if (++st == S) { st = 0; ph ^= 1u; }
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
-    } else if (warp == 12) {
+    } else if constexpr (ROLE == TREE_PRODUCTS) {
+      if (warp == 16) {
       // ------------------------------------------------------------ products
       const uint32_t leader = ptx::elect_one();
       const uint32_t base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
@@ -366,12 +379,22 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
       bool ok = scores(cnt) && (tiles < 2 || scores(cnt + 1));
       for (int i = 0; ok && i < tiles; ++i) {
         const int n = cnt + i, buf = n & 1;
-        if (i + 2 < tiles) {
-          if (!(ok = tc_wait_warp(&aux->read[buf], (n >> 1) & 1, abort_flag))) break;
-          ptx::tc_fence_after();
-          if (!(ok = scores(n + 2))) break;
+        // the stream's next scores or this tile's P V, whichever can go first (a stage may have to be freed by this tile before the next keys come)
+        bool next = i + 2 >= tiles;
+        const long long since = clock64();
+        while (!arrived(&aux->ready[buf], (n >> 1) & 1)) {
+          if (!next && arrived(&aux->read[buf], (n >> 1) & 1) && arrived(&aux->full[(n + 2) % S], (uint32_t)((n + 2) / S) & 1u)) {
+            ptx::tc_fence_after();
+            if (!(ok = scores(n + 2))) break;
+            next = true;
+          }
+          if (__any_sync(0xffffffffu, *abort_flag || clock64() - since > TC_WAIT_LIMIT)) {
+            *abort_flag = 1;
+            ok = false;
+            break;
+          }
         }
-        if (!(ok = tc_wait_warp(&aux->ready[buf], (n >> 1) & 1, abort_flag))) break;
+        if (!ok) break;
         ptx::tc_fence_after();
         const uint32_t v0 = t0 + (n % S) * STAGE + C::T_BYTES;
 #pragma unroll
@@ -379,6 +402,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
           umma_from_tmem(leader, tO + buf * 128, tP + buf * 32 + j * 8, tc_smem_desc(v0 + j * 2048, 8192, 1024), id_o, (i > 1 || j > 0) ? 1u : 0u);
         ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->done[buf]));
         ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->empty[n % S]));
+        if (!next) ok = scores(n + 2);
+      }
       }
     } else {
       // ------------------------------------------------------------ a row a thread, every other tile
@@ -390,88 +415,91 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
       const int i0 = (cnt ^ buf) & 1;                          // the stream's first tile of this item
       for (int i = i0; i < tiles; i += 2) {
         const int n = cnt + i, st = n % S, first = (w.tile + i) * ATTN_UNIT;
-        // (the steps come with the tile, the scores with its product; P and O of the stream's tile before)
-        if (!(ok = tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag) && tc_wait_warp(&aux->scored[buf], (n >> 1) & 1, abort_flag) &&
-                   tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag)))
-          break;
+        // (the steps come with the tile, the scores with its product)
+        if (!(ok = tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag) && tc_wait_warp(&aux->scored[buf], (n >> 1) & 1, abort_flag))) break;
         ptx::tc_fence_after();
         const uint32_t tS = tmem + lanes + buf * 64;
         const unsigned long long bad = (unsigned long long)aux->bad[st][0] | ((unsigned long long)aux->bad[st][1] << 32);
         const bool edge = first + ATTN_UNIT > w.s.context || bad != 0ull;
         const unsigned long long see = edge ? seen64(row.mask, w.s.context, first) & ~bad : ~0ull;
         auto kstep = [&](int j) { return C::BITS == 4 ? *reinterpret_cast<const float4*>(&aux->kstep[st][j]) : make_float4(a.scale, a.scale, a.scale, a.scale); };
+        float s[64];
+        tmem_read64(tS, s);
+        const float neg = m == -INFINITY ? 3e38f : -m;           // (no bound yet: whatever is finite raises it)
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 64; j += 4) {
+          const float4 k = kstep(j);
+          s[j] = fmaf(s[j], k.x, neg); s[j + 1] = fmaf(s[j + 1], k.y, neg); s[j + 2] = fmaf(s[j + 2], k.z, neg); s[j + 3] = fmaf(s[j + 3], k.w, neg);
+        }
+        if (edge) {
+          const uint32_t lo = (uint32_t)see, hi = (uint32_t)(see >> 32);
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (!(((j < 32 ? lo : hi) >> (j & 31)) & 1u)) s[j] = -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < 64; j += 2) top = fmaxf(top, fmaxf(s[j], s[j + 1]));
+        // a score above the bound by 2^8 (there is none yet: any) raises it
+        const bool raise = __any_sync(0xffffffffu, top > 8.f);
+        if (raise) {
+          tmem_read64(tS, s);
+          const uint32_t lo = (uint32_t)see, hi = (uint32_t)(see >> 32);
+          top = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 64; j += 4) {
+            const float4 k = kstep(j);
+            s[j] *= k.x; s[j + 1] *= k.y; s[j + 2] *= k.z; s[j + 3] *= k.w;
+#pragma unroll
+            for (int e = j; e < j + 4; ++e) {
+              if (!(((e < 32 ? lo : hi) >> (e & 31)) & 1u)) s[e] = -INFINITY;
+              top = fmaxf(top, s[e]);
+            }
+          }
+        }
+        ptx::tc_fence_before();
+        ptx::mbar_arrive(&aux->read[buf]);
+        // P and O of the stream's tile before
+        if (!(ok = tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag))) break;
+        ptx::tc_fence_after();
+        if (raise) {
+          const bool up = top > m;                             // (rows below theirs are raised too: no harm)
+          const float f = up ? ex2(m - top) : 1.f;
+          if (up) m = top;
+          l *= f;
+          if (i > i0) {                                        // (the item's first tile overwrites O)
+#pragma unroll 1
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              tmem_read16(tO + buf * 128 + lanes + c, o);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_write16(tO + buf * 128 + lanes + c, o);
+            }
+            tmem_write_wait();
+          }
+          const float bound = m == -INFINITY ? 0.f : m;
+#pragma unroll
+          for (int j = 0; j < 64; ++j) s[j] -= bound;          // (not seen: stays -inf)
+        }
         float sum0 = 0.f, sum1 = 0.f;                          // a tile's probabilities by themselves: fewer roundings of a long sum
-        // 32 columns at a time; where a score exceeds the bound (none yet: any does) the bound is raised and the tile begins again
+#pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float s[32];
-          ptx::tmem_ld32(tS + h * 32, s);
-          const float neg = m == -INFINITY ? INFINITY : -m;
-          float top = -INFINITY;
-#pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            const float4 k = kstep(h * 32 + j);
-            s[j] = fmaf(s[j], k.x, neg); s[j + 1] = fmaf(s[j + 1], k.y, neg); s[j + 2] = fmaf(s[j + 2], k.z, neg); s[j + 3] = fmaf(s[j + 3], k.w, neg);
-          }
-          if (edge) {
-            const uint32_t bits = (uint32_t)(see >> (h * 32));
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!((bits >> j) & 1u)) s[j] = -INFINITY;
-          }
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(s[j], s[j + 1]));
-          if (__any_sync(0xffffffffu, top > 8.f)) {
-            top = -INFINITY;
-#pragma unroll 1
-            for (int g = 0; g < 2; ++g) {
-              ptx::tmem_ld32(tS + g * 32, s);
-              const uint32_t bits = (uint32_t)(see >> (g * 32));
-#pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const float4 k = kstep(g * 32 + j);
-                if (bits & (1u << j)) top = fmaxf(top, s[j] * k.x);
-                if (bits & (2u << j)) top = fmaxf(top, s[j + 1] * k.y);
-                if (bits & (4u << j)) top = fmaxf(top, s[j + 2] * k.z);
-                if (bits & (8u << j)) top = fmaxf(top, s[j + 3] * k.w);
-              }
-            }
-            const bool up = top > m;                           // (rows below theirs are raised too: no harm)
-            const float f = up ? ex2(m - top) : 1.f;
-            if (up) m = top;
-            l *= f;
-            if (i > i0) {                                      // (the item's first tile overwrites O)
-#pragma unroll 1
-              for (int c = 0; c < D; c += 16) {
-                uint32_t o[16];
-                tmem_read16(tO + buf * 128 + lanes + c, o);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                tmem_write16(tO + buf * 128 + lanes + c, o);
-              }
-              tmem_write_wait();
-            }
-            sum0 = sum1 = 0.f;
-            h = -1;
-            continue;
-          }
-          if (h == 1) {
-            ptx::tc_fence_before();
-            ptx::mbar_arrive(&aux->read[buf]);
-          }
           uint32_t p[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
-            float e0 = ex2(s[j]), e1 = ex2(s[j + 1]), e2 = ex2(s[j + 2]), e3 = ex2(s[j + 3]);
+            const int q = h * 32 + j;
+            float e0 = ex2(s[q]), e1 = ex2(s[q + 1]), e2 = ex2(s[q + 2]), e3 = ex2(s[q + 3]);
             sum0 += e0 + e2;
             sum1 += e1 + e3;
             if (C::BITS == 4) {
-              const float4 v = *reinterpret_cast<const float4*>(&aux->vstep[st][h * 32 + j]);
+              const float4 v = *reinterpret_cast<const float4*>(&aux->vstep[st][q]);
               e0 *= v.x; e1 *= v.y; e2 *= v.z; e3 *= v.w;
               if (edge) {                                      // an unseen record may say NaN
-                if (s[j] == -INFINITY) e0 = 0.f;
-                if (s[j + 1] == -INFINITY) e1 = 0.f;
-                if (s[j + 2] == -INFINITY) e2 = 0.f;
-                if (s[j + 3] == -INFINITY) e3 = 0.f;
+                if (s[q] == -INFINITY) e0 = 0.f;
+                if (s[q + 1] == -INFINITY) e1 = 0.f;
+                if (s[q + 2] == -INFINITY) e2 = 0.f;
+                if (s[q + 3] == -INFINITY) e3 = 0.f;
               }
             }
             p[j / 2] = bf16x2(e0, e1);
@@ -609,10 +637,62 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
     head_of_run = false;
     more = w.next(a);
   }
+}
+
+template <typename C>
+__global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* sT = smem;                                          // stages of keys, values
+  uint8_t* sRaw = sT + 2 * C::STAGES * C::T_BYTES;
+  TreeAux<C>* aux = reinterpret_cast<TreeAux<C>*>(sRaw + (C::BITS == 4 ? 2 * C::RAW * C::RAW_BYTES : 0));
+  static_assert(sizeof(TreeAux<C>) <= C::AUX_BYTES, "TreeCfg::AUX_BYTES");
+  constexpr int S = C::STAGES;
+  const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
+  volatile int* abort_flag = &aux->abort_flag;
+  if (tid == 0) {
+    for (int i = 0; i < S; ++i) {
+      ptx::mbar_init(&aux->full[i], 128);
+      ptx::mbar_init(&aux->empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&aux->scored[i], 1);
+      ptx::mbar_init(&aux->read[i], 128);
+      ptx::mbar_init(&aux->ready[i], 128);
+      ptx::mbar_init(&aux->done[i], 1);
+    }
+    aux->abort_flag = 0;
+    ptx::fence_barrier_init();
+    ptx::fence_proxy_async();
+  }
+  if (warp == 0) {
+    Walk<C> b;
+    b.begin(a);
+    if (lane == 0) aux->w = b;
+  }
+  if (warp == 16) {
+    ptx::tmem_alloc(&aux->tmem, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  // The block's registers are shared out again: 2 x 144 + 2 x 72 + 48 = 5 x 96, what it was launched with
+  static_assert(C::THREADS == 640, "five groups of four warps at 96 registers");
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    tree_role<C, TREE_ROWS>(a, aux, sT, sRaw, warp);
+  } else if (warp < 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    tree_role<C, TREE_BRING>(a, aux, sT, sRaw, warp);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    tree_role<C, TREE_PRODUCTS>(a, aux, sT, sRaw, warp);
+  }
   if (tid == 0 && *abort_flag) atomicOr(a.flags, KV_FLAG_TIMEOUT);
   ptx::tc_fence_before();
   __syncthreads();
-  if (warp == 12) ptx::tmem_dealloc(tmem, 512);
+  if (warp == 16) ptx::tmem_dealloc(aux->tmem, 512);
 }
 
 }  // namespace kv
