@@ -82,6 +82,32 @@ __device__ __forceinline__ void umma_from_tmem(uint32_t leader, uint32_t tmem_d,
       ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(leader)
       : "memory");
 }
+// Two fp32 in one instruction.
+__device__ __forceinline__ uint64_t two(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 apart(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t two_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t two_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t two_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 // One look at a barrier, without the hardware's suspension of a waiting thread; the whole warp agrees.
 __device__ __forceinline__ bool arrived(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
@@ -181,7 +207,7 @@ struct Bring {
       if (x) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
     }
   }
-  __device__ __forceinline__ void put(const AttnArgs& a, TreeAux<C>* aux, uint8_t* tile_mem, const uint8_t* raw, int slot, int st, int tid) {
+  __device__ __forceinline__ void put(const AttnArgs& a, TreeAux<C>* aux, uint8_t* tile_mem, const uint8_t* raw, int slot, int st, int tid, bool drafted) {
     uint8_t* kd = tile_mem + plane * 8192 + tok * 128;
     uint8_t* vd = kd + C::T_BYTES;
     const uint8_t* from = raw + slot * C::RAW_BYTES + tid * 16;
@@ -190,7 +216,15 @@ struct Bring {
     if (keys) spread(kd, *reinterpret_cast<const uint4*>(from), *reinterpret_cast<const uint4*>(from + 2048), zero_bias(rec.x), tok);
     if (values) spread(vd, *reinterpret_cast<const uint4*>(from + 4096), *reinterpret_cast<const uint4*>(from + 6144), zero_bias(rec.y), tok);
     if (tid < 64) aux->kstep[st][tok] = step_of(rec.x) * a.scale;                // the scale has the 64 of the codes
-    else aux->vstep[st][tok] = step_of(rec.y) * 64.f;
+    else {
+      // a step that is not finite must not meet the zeros of rows that do not see it: left out here, added at the end
+      float step = step_of(rec.y) * 64.f;
+      if (drafted && !(fabsf(step) < INFINITY)) {
+        step = 0.f;
+        *reinterpret_cast<volatile int*>(&aux->odd) = 1;
+      }
+      aux->vstep[st][tok] = step;
+    }
   }
   // 16 bits: the copies of a tile (one group of copies): eight threads a row of 128 bytes, sixteen rows at a time
   __device__ __forceinline__ void copy(const AttnArgs& a, uint8_t* tile_mem, int tile, int tid) {
@@ -347,7 +381,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
           }
         } else {
           asm volatile("cp.async.wait_group %0;" ::"n"(C::RAW - 1) : "memory");
-          in.put(a, aux, mem, raw, slot, st, id);
+          in.put(a, aux, mem, raw, slot, st, id, (w.tile + i + 1) * ATTN_UNIT > w.s.context);
           if (id < 64) in.lost(a, aux, st, w.tile + i, (in.goods >> slot) & 1u, id >> 5, id);
           ptx::fence_proxy_async();
           ptx::mbar_arrive(&aux->full[st]);
@@ -382,19 +416,18 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         // the stream's next scores or this tile's P V, whichever can go first (a stage may have to be freed by this tile before the next keys come)
         bool next = i + 2 >= tiles;
         const long long since = clock64();
-        while (!arrived(&aux->ready[buf], (n >> 1) & 1)) {
-          if (!next && arrived(&aux->read[buf], (n >> 1) & 1) && arrived(&aux->full[(n + 2) % S], (uint32_t)((n + 2) / S) & 1u)) {
+        while (!next && !arrived(&aux->ready[buf], (n >> 1) & 1)) {
+          if (arrived(&aux->read[buf], (n >> 1) & 1) && arrived(&aux->full[(n + 2) % S], (uint32_t)((n + 2) / S) & 1u)) {
             ptx::tc_fence_after();
             if (!(ok = scores(n + 2))) break;
             next = true;
-          }
-          if (__any_sync(0xffffffffu, *abort_flag || clock64() - since > TC_WAIT_LIMIT)) {
+          } else if (__any_sync(0xffffffffu, *abort_flag || clock64() - since > TC_WAIT_LIMIT)) {
             *abort_flag = 1;
             ok = false;
             break;
           }
         }
-        if (!ok) break;
+        if (!(ok = ok && tc_wait_warp(&aux->ready[buf], (n >> 1) & 1, abort_flag))) break;
         ptx::tc_fence_after();
         const uint32_t v0 = t0 + (n % S) * STAGE + C::T_BYTES;
 #pragma unroll
@@ -422,40 +455,42 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         const unsigned long long bad = (unsigned long long)aux->bad[st][0] | ((unsigned long long)aux->bad[st][1] << 32);
         const bool edge = first + ATTN_UNIT > w.s.context || bad != 0ull;
         const unsigned long long see = edge ? seen64(row.mask, w.s.context, first) & ~bad : ~0ull;
-        auto kstep = [&](int j) { return C::BITS == 4 ? *reinterpret_cast<const float4*>(&aux->kstep[st][j]) : make_float4(a.scale, a.scale, a.scale, a.scale); };
-        float s[64];
-        tmem_read64(tS, s);
-        const float neg = m == -INFINITY ? 3e38f : -m;           // (no bound yet: whatever is finite raises it)
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 64; j += 4) {
-          const float4 k = kstep(j);
-          s[j] = fmaf(s[j], k.x, neg); s[j + 1] = fmaf(s[j + 1], k.y, neg); s[j + 2] = fmaf(s[j + 2], k.z, neg); s[j + 3] = fmaf(s[j + 3], k.w, neg);
-        }
-        if (edge) {
+        const uint64_t all = two(a.scale, a.scale);
+        auto kstep = [&](int j) { return C::BITS == 4 ? *reinterpret_cast<const ulonglong2*>(&aux->kstep[st][j]) : make_ulonglong2(all, all); };
+        auto blind = [&](float (&s)[64]) {                     // not seen: -inf
           const uint32_t lo = (uint32_t)see, hi = (uint32_t)(see >> 32);
 #pragma unroll
           for (int j = 0; j < 64; ++j)
             if (!(((j < 32 ? lo : hi) >> (j & 31)) & 1u)) s[j] = -INFINITY;
+        };
+        float s[64];
+        tmem_read64(tS, s);
+        const float neg = m == -INFINITY ? 3e38f : -m;         // (no bound yet: whatever is finite raises it)
+        const uint64_t neg2 = two(neg, neg);
+#pragma unroll
+        for (int j = 0; j < 64; j += 4) {
+          const ulonglong2 k = kstep(j);
+          const float2 x = apart(two_fma(two(s[j], s[j + 1]), k.x, neg2)), y = apart(two_fma(two(s[j + 2], s[j + 3]), k.y, neg2));
+          s[j] = x.x; s[j + 1] = x.y; s[j + 2] = y.x; s[j + 3] = y.y;
         }
+        if (edge) blind(s);
+        float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 64; j += 2) top = fmaxf(top, fmaxf(s[j], s[j + 1]));
         // a score above the bound by 2^8 (there is none yet: any) raises it
         const bool raise = __any_sync(0xffffffffu, top > 8.f);
         if (raise) {
           tmem_read64(tS, s);
-          const uint32_t lo = (uint32_t)see, hi = (uint32_t)(see >> 32);
           top = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 64; j += 4) {
-            const float4 k = kstep(j);
-            s[j] *= k.x; s[j + 1] *= k.y; s[j + 2] *= k.z; s[j + 3] *= k.w;
-#pragma unroll
-            for (int e = j; e < j + 4; ++e) {
-              if (!(((e < 32 ? lo : hi) >> (e & 31)) & 1u)) s[e] = -INFINITY;
-              top = fmaxf(top, s[e]);
-            }
+            const ulonglong2 k = kstep(j);
+            const float2 x = apart(two_mul(two(s[j], s[j + 1]), k.x)), y = apart(two_mul(two(s[j + 2], s[j + 3]), k.y));
+            s[j] = x.x; s[j + 1] = x.y; s[j + 2] = y.x; s[j + 3] = y.y;
           }
+          blind(s);
+#pragma unroll
+          for (int j = 0; j < 64; j += 2) top = fmaxf(top, fmaxf(s[j], s[j + 1]));
         }
         ptx::tc_fence_before();
         ptx::mbar_arrive(&aux->read[buf]);
@@ -482,32 +517,28 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
 #pragma unroll
           for (int j = 0; j < 64; ++j) s[j] -= bound;          // (not seen: stays -inf)
         }
-        float sum0 = 0.f, sum1 = 0.f;                          // a tile's probabilities by themselves: fewer roundings of a long sum
+        uint64_t sum = two(0.f, 0.f);                          // a tile's probabilities by themselves: fewer roundings of a long sum
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t p[16];
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
             const int q = h * 32 + j;
-            float e0 = ex2(s[q]), e1 = ex2(s[q + 1]), e2 = ex2(s[q + 2]), e3 = ex2(s[q + 3]);
-            sum0 += e0 + e2;
-            sum1 += e1 + e3;
+            uint64_t x = two(ex2(s[q]), ex2(s[q + 1])), y = two(ex2(s[q + 2]), ex2(s[q + 3]));
+            sum = two_add(two_add(sum, x), y);
             if (C::BITS == 4) {
-              const float4 v = *reinterpret_cast<const float4*>(&aux->vstep[st][q]);
-              e0 *= v.x; e1 *= v.y; e2 *= v.z; e3 *= v.w;
-              if (edge) {                                      // an unseen record may say NaN
-                if (s[q] == -INFINITY) e0 = 0.f;
-                if (s[q + 1] == -INFINITY) e1 = 0.f;
-                if (s[q + 2] == -INFINITY) e2 = 0.f;
-                if (s[q + 3] == -INFINITY) e3 = 0.f;
-              }
+              const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(&aux->vstep[st][q]);
+              x = two_mul(x, v.x);
+              y = two_mul(y, v.y);
             }
-            p[j / 2] = bf16x2(e0, e1);
-            p[j / 2 + 1] = bf16x2(e2, e3);
+            const float2 e = apart(x), f = apart(y);
+            p[j / 2] = bf16x2(e.x, e.y);
+            p[j / 2 + 1] = bf16x2(f.x, f.y);
           }
           tmem_write16(tP + lanes + buf * 32 + h * 16, p);
         }
-        l += sum0 + sum1;
+        const float2 sums = apart(sum);
+        l += sums.x + sums.y;
         tmem_write_wait();
         ptx::tc_fence_before();
         ptx::mbar_arrive(&aux->ready[buf]);
@@ -534,7 +565,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
           f[1] *= inv;
         }
         const int only = (cnt & 1);                            // the stream of the item's first tile
-        const int odd = C::BITS == 16 ? *reinterpret_cast<volatile int*>(&aux->odd) : 0;
+        const int odd = *reinterpret_cast<volatile int*>(&aux->odd);
 #pragma unroll 1
         for (int c = buf * (D / 2); c < (buf + 1) * (D / 2); c += 32) {
           float o[32];
@@ -547,7 +578,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
 #pragma unroll
             for (int j = 0; j < 32; ++j) o[j] = fmaf(x[j], f[only ^ 1], o[j]);
           }
-          if (C::BITS == 16 && odd && row.real) {
+          if (odd && row.real) {
             // values that are not finite, of the tokens that the row sees (rare)
             for (int pos = max(w.tile * ATTN_UNIT, w.s.context & ~(ATTN_UNIT - 1)); pos < min(len, w.end * ATTN_UNIT); ++pos) {
               const int d = pos - w.s.context;
@@ -555,7 +586,16 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
               const int page = (pos >> a.log_page) < a.table_width ? a.table[(long long)w.b * a.table_stride + (pos >> a.log_page)] : -1;
               if ((unsigned)page >= (unsigned)a.pages) continue;
               const int at = pos & (a.page_size - 1);
-              const uint8_t* v = a.cache + (long long)page * a.page_bytes + (long long)(w.item % a.kv_heads) * a.block_bytes + (PL + c / 64) * a.plane_bytes + at * 128;
+              const uint8_t* v = a.cache + (long long)page * a.page_bytes + (long long)(w.item % a.kv_heads) * a.block_bytes;
+              if (C::BITS == 4) {
+                const float step = step_of(*reinterpret_cast<const uint32_t*>(v + 2 * a.codes_bytes + (a.page_size + at) * 4));
+                if (!(fabsf(step) < INFINITY)) {
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) o[j] = __uint_as_float(0x7FC00000u);
+                }
+                continue;
+              }
+              v += (PL + c / 64) * a.plane_bytes + at * 128;
 #pragma unroll
               for (int j = 0; j < 32; ++j) {
                 const int e = (c & 63) + j;
@@ -642,7 +682,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
 template <typename C>
 __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs a) {
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* smem = smem_raw + (-ptx::smem_u32(smem_raw) & 1023u);         // (by an offset: the compiler goes on knowing that this is shared memory)
   uint8_t* sT = smem;                                          // stages of keys, values
   uint8_t* sRaw = sT + 2 * C::STAGES * C::T_BYTES;
   TreeAux<C>* aux = reinterpret_cast<TreeAux<C>*>(sRaw + (C::BITS == 4 ? 2 * C::RAW * C::RAW_BYTES : 0));
