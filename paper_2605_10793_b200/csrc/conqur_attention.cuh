@@ -49,6 +49,7 @@ constexpr int ATTN_CHUNK = 32;                                   // tokens a war
 template <int BITS_, int D_, int NT_, int WN_, int STAGES_, int PER_SM_>
 struct AttnCfg {
   static constexpr int BITS = BITS_, D = D_, NT = NT_, WN = WN_, STAGES = STAGES_, PER_SM = PER_SM_;
+  static constexpr int MIN_RUN = 1;
   static constexpr int THREADS = 32 * WN;
   static constexpr int ROWS = 8 * NT;                            // query rows of a block
   static constexpr int STAGE_BYTES = ATTN_CHUNK * (BITS == 4 ? D + 8 : 4 * D);
@@ -157,7 +158,7 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
 template <typename C>
 struct Walk {
   long long left, total, at;         // tiles of the run still to come; of all work; the next tile's place in all work
-  int ctas;                          // CTAs with a run: no more than there are tiles, so that none is empty
+  int ctas;                          // CTAs with a run: none is empty
   Seq s;
   int b, item, tile;                 // the item's sequence, its number there (block of rows * kv_heads + key head), and its next tile
   int end;                           // the run's last tile of the item, plus one
@@ -173,7 +174,7 @@ struct Walk {
     }
 #pragma unroll
     for (int m = 16; m >= 1; m >>= 1) total += __shfl_xor_sync(0xffffffffu, total, m);
-    ctas = total < (long long)gridDim.x ? (int)total : (int)gridDim.x;
+    ctas = (int)min((long long)gridDim.x, (total + C::MIN_RUN - 1) / C::MIN_RUN);
     b = 0;
     left = 0;
     if ((int)blockIdx.x >= ctas) return;

@@ -16,6 +16,8 @@
 namespace conqur {
 namespace kv {
 
+enum { BAR_ITEM = 5 };
+
 template <int BITS_, int D_>
 struct TreeCfg {
   static constexpr int BITS = BITS_, D = D_;
@@ -27,6 +29,7 @@ struct TreeCfg {
   // TMEM columns: scores 2 x 64, accumulators 2 x 128, the rows D / 2 (two bf16 a column), probabilities 2 x 32
   static constexpr int T_O = 128, T_Q = 384, T_P = 448;
   static_assert(SMEM <= 227 * 1024, "shared memory of an SM");
+  static constexpr int MIN_RUN = 4;                            // tiles a CTA takes at least
   static constexpr int SLOT = (D + 2) * 128;                   // floats of a part: columns of 128 rows; then bounds, sums
 };
 
@@ -38,7 +41,9 @@ struct TreeAux {
   float bound[2][128], sum[2][128];                            // of the two streams
   Walk<C> w;
   uint32_t tmem;
-  int abort_flag, last, odd;                                   // odd: some value near the end of the sequence is not finite
+  int abort_flag, last;
+  int odd;                                                     // some value or step of a drafted token was not finite (never taken back: it only asks for a look)
+  int stop[2];                                                 // abort_flag as all warps of the rows and the products see it, at an item's start and end
 };
 
 // 32 lanes x 16 consecutive columns: thread t of the warp holds row (lane base + t).
@@ -323,12 +328,15 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         }
         tmem_write16(tQ + ((uint32_t)(warp * 32) << 16) + c, x);
       }
-      if (tid == 0) aux->odd = 0;
+      if (tid == 0) aux->stop[0] = *abort_flag;
       tmem_write_wait();
       ptx::tc_fence_before();
     }
-    __syncthreads();
-    ptx::tc_fence_after();
+    if constexpr (ROLE != TREE_BRING) {                        // (keys and values run ahead into the next item)
+      bar_sync(BAR_ITEM, 288);
+      if (*reinterpret_cast<volatile int*>(&aux->stop[0])) break;
+      ptx::tc_fence_after();
+    }
     const int tiles = w.end - w.tile;
     const int len = w.s.context + w.s.nodes;
 
@@ -393,7 +401,6 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
     } else if constexpr (ROLE == TREE_PRODUCTS) {
-      if (warp == 16) {
       // ------------------------------------------------------------ products
       const uint32_t leader = ptx::elect_one();
       const uint32_t base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
@@ -436,7 +443,6 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->done[buf]));
         ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->empty[n % S]));
         if (!next) ok = scores(n + 2);
-      }
       }
     } else {
       // ------------------------------------------------------------ a row a thread, every other tile
@@ -548,8 +554,9 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       ptx::tc_fence_after();
       aux->bound[buf][r] = m;
       aux->sum[buf][r] = l;
+      if (tid == 0) aux->stop[1] = *abort_flag;
       bar_sync(BAR_ALL, 256);
-      if (!*abort_flag) {
+      if (!*reinterpret_cast<volatile int*>(&aux->stop[1])) {
         const bool whole = w.tile == 0 && w.end == w.s.tiles;
         // the two streams together; each group of warps takes half of the columns
         const float m0 = aux->bound[0][r], m1 = aux->bound[1][r];
@@ -652,17 +659,21 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
             const bool zero = tl == 0.f && tm == -INFINITY;
             const float ti = zero ? 0.f : 1.f / tl;
 #pragma unroll 1
-            for (int c = buf * (D / 2); c < (buf + 1) * (D / 2); c += 8) {
-              float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+            for (int c = buf * (D / 2); c < (buf + 1) * (D / 2); c += 32) {
+              float o[32] = {};
+#pragma unroll 2
               for (int k = c0; k <= c1; ++k) {
                 const float* p = slot(k);
                 const float om = __ldcg(p + D * 128), f = (tm == -INFINITY ? 1.f : ex2(om - tm)) * ti;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = fmaf(__ldcg(p + (c + j) * 128), f, o[j]);
+                for (int j = 0; j < 32; ++j) o[j] = fmaf(__ldcg(p + (c + j) * 128), f, o[j]);
               }
-              if (row.real)
-                *reinterpret_cast<uint4*>(a.out + row.row * a.o_t + row.head * a.o_h + c) = make_uint4(bf16x2(o[0], o[1]), bf16x2(o[2], o[3]), bf16x2(o[4], o[5]), bf16x2(o[6], o[7]));
+              if (row.real) {
+                __nv_bfloat16* out = a.out + row.row * a.o_t + row.head * a.o_h + c;
+#pragma unroll
+                for (int j = 0; j < 32; j += 8)
+                  *reinterpret_cast<uint4*>(out + j) = make_uint4(bf16x2(o[j], o[j + 1]), bf16x2(o[j + 2], o[j + 3]), bf16x2(o[j + 4], o[j + 5]), bf16x2(o[j + 6], o[j + 7]));
+              }
             }
             if (buf == 0 && row.real && a.lse) a.lse[row.row * a.lse_t + row.head] = zero ? -INFINITY : (tm == -INFINITY ? 0.f : tm) * 0.6931471805599453f + logf(tl);
           }
@@ -670,9 +681,11 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       }
       ptx::tc_fence_before();
     }
-    __syncthreads();                                           // rows, tiles and accumulators may be replaced
-    ptx::tc_fence_after();
-    if (*abort_flag) break;
+    if constexpr (ROLE != TREE_BRING) {
+      bar_sync(BAR_ITEM, 288);                                 // rows and accumulators may be replaced
+    } else {
+      if (__any_sync(0xffffffffu, *abort_flag)) break;
+    }
     cnt += tiles;
     head_of_run = false;
     more = w.next(a);
@@ -701,7 +714,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
       ptx::mbar_init(&aux->ready[i], 128);
       ptx::mbar_init(&aux->done[i], 1);
     }
-    aux->abort_flag = 0;
+    aux->abort_flag = aux->odd = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async();
   }
@@ -727,7 +740,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
     tree_role<C, TREE_BRING>(a, aux, sT, sRaw, warp);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    tree_role<C, TREE_PRODUCTS>(a, aux, sT, sRaw, warp);
+    if (warp == 16) tree_role<C, TREE_PRODUCTS>(a, aux, sT, sRaw, warp);
   }
   if (tid == 0 && *abort_flag) atomicOr(a.flags, KV_FLAG_TIMEOUT);
   ptx::tc_fence_before();
