@@ -40,26 +40,28 @@ struct RowsArgs {
 
 constexpr int ROWS_THREADS = 256;
 
-
-// Step, zero-point code and codes of a row whose lanes hold eight elements each; L lanes a row.
-template <int L, bool CLIP>
-__device__ __forceinline__ void quantise(const uint4 raw, float clip, uint32_t& word, uint32_t& record) {
+// max and -min of a lane's eight elements as a pair of bf16, NaN kept
+__device__ __forceinline__ uint32_t range_of(const uint4 raw) {
   const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-  // (max, -min) as a pair of bf16, NaN kept
-  __nv_bfloat162 h[4], mx, mn;
+  __nv_bfloat162 h[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) h[i] = *reinterpret_cast<const __nv_bfloat162*>(&w[i]);
-  mx = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-  mn = __hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3]));
-  __nv_bfloat162 both = __halves2bfloat162(__hmax_nan(__low2bfloat16(mx), __high2bfloat16(mx)),
-                                           __hneg(__hmin_nan(__low2bfloat16(mn), __high2bfloat16(mn))));
-#pragma unroll
-  for (int m = 1; m < L; m <<= 1) {
-    const uint32_t o = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<uint32_t*>(&both), m);
-    both = __hmax2_nan(both, *reinterpret_cast<const __nv_bfloat162*>(&o));
-  }
-  const float top = __low2float(both), low = -__high2float(both);
-  float step, zero = 0.f, inv = 0.f;
+  const __nv_bfloat162 mx = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  const __nv_bfloat162 mn = __hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3]));
+  const __nv_bfloat162 both = __halves2bfloat162(__hmax_nan(__low2bfloat16(mx), __high2bfloat16(mx)),
+                                                 __hneg(__hmin_nan(__low2bfloat16(mn), __high2bfloat16(mn))));
+  return *reinterpret_cast<const uint32_t*>(&both);
+}
+__device__ __forceinline__ uint32_t wider(uint32_t x, uint32_t y) {
+  const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+// Record (step, zero-point code) and 1 / step (0: all codes are zero) of a row with this range.
+template <bool CLIP>
+__device__ __forceinline__ uint32_t row_record(uint32_t range, float clip, float& inv) {
+  const float top = __uint_as_float(range << 16), low = -__uint_as_float(range & 0xFFFF0000u);
+  float step, zero = 0.f;
+  inv = 0.f;
   if (!(top < 1.7014118346046923e38f && low > -1.7014118346046923e38f)) {      // 2^127: a code's value may lie 1/15 beyond the range
     step = __uint_as_float(0x7FC00000u);
   } else {
@@ -78,19 +80,46 @@ __device__ __forceinline__ void quantise(const uint4 raw, float clip, uint32_t& 
       inv = 1.f / step;
     }
   }
-  const int bias = (int)zero - 0x4B400000;
-  int code[8];
+  return (__float_as_uint(step) >> 16) | ((uint32_t)zero << 16);
+}
+// A lane's eight codes.
+template <bool CLIP>
+__device__ __forceinline__ uint32_t row_codes(const uint4 raw, uint32_t record, float inv) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w}, zeros = (record >> 16) * 0x10001u;
+  const uint64_t inv2 = kv::two(inv, inv), up = kv::two(6144.f, 6144.f), down = kv::two(-6144.f, -6144.f), magic = kv::two(12582912.f, 12582912.f);
+  uint32_t c[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = __uint_as_float((i & 1) ? (w[i >> 1] & 0xFFFF0000u) : (w[i >> 1] << 16));
-    float q;
-    if (CLIP) q = (fminf(fmaxf(y * inv, -64.f), 64.f) + 6144.f) - 6144.f;      // 1.5 * 2^12: multiples of 2^-11
-    else q = fmaf(y, inv, 6144.f) - 6144.f;
-    code[i] = min(max(__float_as_int(q + 12582912.f) + bias, 0), 15);          // 1.5 * 2^23: half to even
+  for (int i = 0; i < 4; ++i) {
+    uint64_t q = kv::two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+    if (CLIP) {                                                // (beyond the range by any factor)
+      const float2 y = kv::apart(kv::two_mul(q, inv2));
+      q = kv::two_add(kv::two(fminf(fmaxf(y.x, -64.f), 64.f), fminf(fmaxf(y.y, -64.f), 64.f)), up);
+    } else {
+      q = kv::two_fma(q, inv2, up);                            // 1.5 * 2^12: multiples of 2^-11
+    }
+    const float2 r = kv::apart(kv::two_add(kv::two_add(q, down), magic));      // 1.5 * 2^23: half to even, the integer in the low bits
+    c[i] = __viaddmin_s16x2_relu(__byte_perm(__float_as_uint(r.x), __float_as_uint(r.y), 0x5410), zeros, 0x000F000Fu);
   }
-  word = (uint32_t)(code[0] | (code[2] << 4) | (code[4] << 8) | (code[6] << 12) | (code[1] << 16) | (code[3] << 20) | (code[5] << 24) | (code[7] << 28));
-  if (!(step > 0.f)) word = 0u;
-  record = (__float_as_uint(step) >> 16) | ((uint32_t)zero << 16);
+  return inv > 0.f ? c[0] | (c[1] << 4) | (c[2] << 8) | (c[3] << 12) : 0u;
+}
+// Four rows, L lanes each with eight elements of every one.  The ranges are reduced so that a lane ends with that of row lane % 4: the divisions of a row
+// are made by L / 4 lanes, not L, and handed round.
+template <int L, bool CLIP>
+__device__ __forceinline__ void quantise4(const uint4 (&raw)[4], float clip, int l, uint32_t (&word)[4], uint32_t (&record)[4]) {
+  const uint32_t r0 = range_of(raw[0]), r1 = range_of(raw[1]), r2 = range_of(raw[2]), r3 = range_of(raw[3]);
+  const bool b0 = l & 1, b1 = l & 2;
+  const uint32_t x = wider(b0 ? r1 : r0, __shfl_xor_sync(0xffffffffu, b0 ? r0 : r1, 1));
+  const uint32_t y = wider(b0 ? r3 : r2, __shfl_xor_sync(0xffffffffu, b0 ? r2 : r3, 1));
+  uint32_t range = wider(b1 ? y : x, __shfl_xor_sync(0xffffffffu, b1 ? x : y, 2));
+#pragma unroll
+  for (int m = 4; m < L; m <<= 1) range = wider(range, __shfl_xor_sync(0xffffffffu, range, m));
+  float inv;
+  const uint32_t rec = row_record<CLIP>(range, clip, inv);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    record[r] = __shfl_sync(0xffffffffu, rec, r, 4);
+    word[r] = row_codes<CLIP>(raw[r], record[r], __shfl_sync(0xffffffffu, inv, r, 4));
+  }
 }
 
 template <bool VEC>
@@ -111,29 +140,26 @@ __global__ void __launch_bounds__(ROWS_THREADS) kv_append_kernel(const RowsArgs 
   constexpr int L = D / 8, PER_BLOCK = ROWS_THREADS / L;
   const int l = threadIdx.x % L;
   const int64_t first = (int64_t)blockIdx.x * PER_BLOCK * 2 + threadIdx.x / L;
-  uint4 kr[2], vr[2];
+  uint4 rows[4];                                               // key and value of both items
   int64_t slot[2];
   int head[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int64_t item = first + u * PER_BLOCK;
     slot[u] = -1;
-    kr[u] = vr[u] = make_uint4(0u, 0u, 0u, 0u);
+    rows[2 * u] = rows[2 * u + 1] = make_uint4(0u, 0u, 0u, 0u);
     if (item < a.items) {
       int64_t token;
       split_item(a, item, token, head[u]);
       slot[u] = a.slots[token];
-      kr[u] = load8<VEC>(a.k + token * a.k_t + head[u] * a.k_h + 8 * l);
-      vr[u] = load8<VEC>(a.v + token * a.v_t + head[u] * a.v_h + 8 * l);
+      rows[2 * u] = load8<VEC>(a.k + token * a.k_t + head[u] * a.k_h + 8 * l);
+      rows[2 * u + 1] = load8<VEC>(a.v + token * a.v_t + head[u] * a.v_h + 8 * l);
     }
   }
+  uint32_t word[4], record[4];
+  if (BITS == 4) quantise4<L, CLIP>(rows, a.clip, l, word, record);      // all lanes: there are shuffles
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    uint32_t kw, krec, vw, vrec;
-    if (BITS == 4) {                                           // all lanes: the rows' ranges are found with shuffles
-      quantise<L, CLIP>(kr[u], a.clip, kw, krec);
-      quantise<L, CLIP>(vr[u], a.clip, vw, vrec);
-    }
     if (slot[u] < 0) continue;
     if (slot[u] >= a.slots_total) {
       if (l == 0) atomicOr(a.flags, kv::KV_FLAG_BAD_INDEX);
@@ -143,13 +169,13 @@ __global__ void __launch_bounds__(ROWS_THREADS) kv_append_kernel(const RowsArgs 
     const int ps = 1 << a.log_page, t = (int)(slot[u] & (ps - 1));
     uint8_t* block = a.cache + (page * a.heads + head[u]) * a.block_bytes;
     if (BITS == 4) {
-      *reinterpret_cast<uint32_t*>(block + t * (D / 2) + 4 * l) = kw;
-      *reinterpret_cast<uint32_t*>(block + (ps + t) * (D / 2) + 4 * l) = vw;
-      if (l < 2) *reinterpret_cast<uint32_t*>(block + ps * D + (l * ps + t) * 4) = l ? vrec : krec;
+      *reinterpret_cast<uint32_t*>(block + t * (D / 2) + 4 * l) = word[2 * u];
+      *reinterpret_cast<uint32_t*>(block + (ps + t) * (D / 2) + 4 * l) = word[2 * u + 1];
+      if (l < 2) *reinterpret_cast<uint32_t*>(block + ps * D + (l * ps + t) * 4) = l ? record[2 * u + 1] : record[2 * u];
     } else {
       const int at = ((l >> 3) * ps + t) * 128 + (((l & 7) ^ (t & 7)) << 4);
-      *reinterpret_cast<uint4*>(block + at) = kr[u];
-      *reinterpret_cast<uint4*>(block + ps * D * 2 + at) = vr[u];
+      *reinterpret_cast<uint4*>(block + at) = rows[2 * u];
+      *reinterpret_cast<uint4*>(block + ps * D * 2 + at) = rows[2 * u + 1];
     }
   }
 }
@@ -162,10 +188,19 @@ __device__ __forceinline__ void store8(bf16* p, const float (&x)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(kv::bf16x2(x[0], x[1]), kv::bf16x2(x[2], x[3]), kv::bf16x2(x[4], x[5]), kv::bf16x2(x[6], x[7]));
 }
 
+// (code - zero-point) * step: a code masked where it lies, with the bits of 2^23 above it, is 2^23 + c 16^i; every step but the last product is exact.
 __device__ __forceinline__ void unpack(uint32_t w, uint32_t record, float (&x)[8]) {
-  const float step = kv::step_of(record), zero = (float)kv::zero_of(record);
+  const float step = kv::step_of(record), z = (float)kv::zero_of(record);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[(i & 3) * 2 + (i >> 2)] = ((float)((w >> (4 * i)) & 15u) - zero) * step;
+  for (int i = 0; i < 4; ++i) {
+    const float p = (float)(1 << (4 * i)), down = -fmaf(z, p, 8388608.f), scaled = step * (1.f / p);
+    const uint32_t m = 15u << (4 * i);
+    const float2 v = kv::apart(kv::two_mul(
+        kv::two_add(kv::two(__uint_as_float((w & m) | 0x4B000000u), __uint_as_float(((w >> 16) & m) | 0x4B000000u)), kv::two(down, down)),
+        kv::two(scaled, scaled)));
+    x[2 * i] = v.x;
+    x[2 * i + 1] = v.y;
+  }
 }
 
 template <int BITS, int D, typename T>
