@@ -49,7 +49,7 @@ constexpr int ATTN_CHUNK = 32;                                   // tokens a war
 template <int BITS_, int D_, int NT_, int WN_, int STAGES_, int PER_SM_>
 struct AttnCfg {
   static constexpr int BITS = BITS_, D = D_, NT = NT_, WN = WN_, STAGES = STAGES_, PER_SM = PER_SM_;
-  static constexpr int MIN_RUN = 1;
+  static constexpr int MIN_RUN = 4;
   static constexpr int THREADS = 32 * WN;
   static constexpr int ROWS = 8 * NT;                            // query rows of a block
   static constexpr int STAGE_BYTES = ATTN_CHUNK * (BITS == 4 ? D + 8 : 4 * D);
@@ -157,24 +157,56 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
 // A CTA's run of tiles, item after item; an item is one (sequence, block of rows, key head).
 template <typename C>
 struct Walk {
-  long long left, total, at;         // tiles of the run still to come; of all work; the next tile's place in all work
+  long long left, total, at;         // tiles of the run still to come; places of all work; the next tile's place
   int ctas;                          // CTAs with a run: none is empty
   Seq s;
   int b, item, tile;                 // the item's sequence, its number there (block of rows * kv_heads + key head), and its next tile
   int end;                           // the run's last tile of the item, plus one
   long long item_at;                 // place of the item's first tile
 
+  int pad;                           // 1, or the length of the runs, of which each item takes a whole number of places
+
+  __device__ int places(int tiles) const { return pad == 1 ? tiles : (int)((unsigned)(tiles + pad - 1) / (unsigned)pad) * pad; }
   // One warp: a sum over the sequences, then the one in which the run begins.
   __device__ void begin(const AttnArgs& a) {
     const int lane = threadIdx.x & 31;
     total = 0;
+    long long items = 0;
+    Seq own = {};                                              // of the first 32 sequences: read once
+    if (lane < a.batch) own = sequence<C>(a, lane);
     for (int i = lane; i < a.batch; i += 32) {
-      const Seq q = sequence<C>(a, i);
+      const Seq q = i < 32 ? own : sequence<C>(a, i);
       total += (long long)q.tiles * q.blocks * a.kv_heads;
+      items += q.tiles ? (long long)q.blocks * a.kv_heads : 0;
     }
 #pragma unroll
-    for (int m = 16; m >= 1; m >>= 1) total += __shfl_xor_sync(0xffffffffu, total, m);
-    ctas = (int)min((long long)gridDim.x, (total + C::MIN_RUN - 1) / C::MIN_RUN);
+    for (int m = 16; m >= 1; m >>= 1) {
+      total += __shfl_xor_sync(0xffffffffu, total, m);
+      items += __shfl_xor_sync(0xffffffffu, items, m);
+    }
+    const int grid = (int)gridDim.x;
+    ctas = (int)min((long long)grid, (total + C::MIN_RUN - 1) / C::MIN_RUN);
+    pad = 1;
+    if (items > 0 && items <= ctas) {
+      // Runs that end with their item, if the grid has enough for it with up to four tiles more each than it would take otherwise: a run over two items
+      // costs its CTA about 6 us, four tiles 2.  (One sequence of 8192, 8 key heads: 22.5 to 16.0 us over 4 bits, 22.7 to 17.4 over bf16.)
+      constexpr int TRY = 2;
+      const int run = max(C::MIN_RUN, (int)ratio(total + grid - 1, grid));
+      int pieces[TRY] = {};
+      for (int i = lane; i < a.batch; i += 32) {
+        const Seq q = i < 32 ? own : sequence<C>(a, i);
+#pragma unroll
+        for (int j = 0; j < TRY; ++j) pieces[j] += min((int)((unsigned)(q.tiles + run + 4 * j - 1) / (unsigned)(run + 4 * j)) * q.blocks * a.kv_heads, grid + 1);
+      }
+#pragma unroll
+      for (int j = TRY - 1; j >= 0; --j) {
+        const int n = __reduce_add_sync(0xffffffffu, min(pieces[j], grid + 1));
+        if (n > grid) continue;
+        pad = run + 4 * j;
+        ctas = n;
+      }
+      if (pad > 1) total = (long long)ctas * pad;
+    }
     b = 0;
     left = 0;
     if ((int)blockIdx.x >= ctas) return;
@@ -184,8 +216,8 @@ struct Walk {
     for (int base = 0; base < a.batch; base += 32) {
       long long mine = 0;
       if (base + lane < a.batch) {
-        const Seq q = sequence<C>(a, base + lane);
-        mine = (long long)q.tiles * q.blocks * a.kv_heads;
+        const Seq q = base == 0 ? own : sequence<C>(a, base + lane);
+        mine = (long long)places(q.tiles) * q.blocks * a.kv_heads;
       }
       long long upto = mine;
 #pragma unroll
@@ -202,11 +234,20 @@ struct Walk {
       }
       before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    s = sequence<C>(a, b);
+    if (b < 32) {
+      s.start = __shfl_sync(0xffffffffu, own.start, b);
+      s.nodes = __shfl_sync(0xffffffffu, own.nodes, b);
+      s.context = __shfl_sync(0xffffffffu, own.context, b);
+      s.tiles = __shfl_sync(0xffffffffu, own.tiles, b);
+      s.blocks = __shfl_sync(0xffffffffu, own.blocks, b);
+    } else {
+      s = sequence<C>(a, b);
+    }
     const long long in_seq = at - before;
-    item = (int)(in_seq / s.tiles);
-    tile = (int)(in_seq - (long long)item * s.tiles);
+    item = (int)ratio(in_seq, places(s.tiles));
+    tile = (int)(in_seq - (long long)item * places(s.tiles));
     item_at = at - tile;
+    if (pad > 1) left = min(left, (long long)(s.tiles - tile));
     cut();
   }
   __device__ void cut() { end = (long long)(s.tiles - tile) <= left ? s.tiles : tile + (int)left; }
@@ -226,8 +267,12 @@ struct Walk {
     return true;
   }
   // CTA whose run holds a tile
-  __device__ int owner(long long t) const { return (int)(((t + 1) * ctas - 1) / total); }
-  __device__ long long run_begin(int cta) const { return total * cta / ctas; }
+  __device__ int owner(long long t) const { return (int)(pad > 1 ? ratio(t, pad) : ratio((t + 1) * ctas - 1, total)); }
+  __device__ long long run_begin(int cta) const { return pad > 1 ? (long long)pad * cta : ratio(total * cta, ctas); }
+  // (64-bit divisions cost several times those of 32 bits: a few of them were 1 us of a call)
+  static __device__ long long ratio(long long x, long long y) {
+    return (((unsigned long long)x | (unsigned long long)y) >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
+  }
 };
 
 // ---------------------------------------------------------------------------------------------- copies
@@ -412,15 +457,15 @@ struct Acc {
   }
 };
 
-// The warps' parts of a block of rows into those of wn = 0, by halves (every warp comes here).
+// The parts of `warps` warps, by halves, into those of the first (every warp of the CTA comes here).
 template <typename C>
-__device__ __forceinline__ void attn_merge(Acc<C>& acc, float* buf, int wn, int lane) {
+__device__ __forceinline__ void attn_merge(Acc<C>& acc, float* buf, int me, int warps, int lane) {
 #pragma unroll 1
-  for (int h = C::WN / 2; h >= 1; h >>= 1) {
-    float* p = buf + (size_t)(wn & (h - 1)) * C::PART * 32 + lane;
-    if (wn >= h && wn < 2 * h) acc.template store<false>(p, 32);
+  for (int h = warps / 2; h >= 1; h >>= 1) {
+    float* p = buf + (size_t)(me & (h - 1)) * C::PART * 32 + lane;
+    if (me >= h && me < 2 * h) acc.template store<false>(p, 32);
     bar_sync(BAR_ALL, C::THREADS);
-    if (wn < h) acc.template add<false>(p, 32);
+    if (me < h) acc.template add<false>(p, 32);
     bar_sync(BAR_ALL, C::THREADS);
   }
 }
@@ -877,14 +922,17 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) attn_kernel(const AttnA
   } while (more);
   if (wn != (adder + C::WN - 1) % C::WN) bar_sync(BAR_ADDED + (turn ^ 1), C::THREADS);
   bar_sync(BAR_ALL, C::THREADS);
-  for (int i = 0; i < aux->todos; ++i) {
-    const auto& d = aux->todo[i];
+  // Cut items whose last part was this CTA's: with two of them half of the warps each.
+  const int todos = aux->todos;
+  if (todos > 0) {
+    const int warps = C::WN / todos, which = wn / warps, me = wn - which * warps;
+    const auto& d = aux->todo[which];
     acc.clear();
-    for (int k = d.c0 + wn; k <= d.c1; k += C::WN)
+    for (int k = d.c0 + me; k <= d.c1; k += warps)
       // the part of CTA k: its run begins with it unless the item began inside the run
       acc.template add<true>(a.parts + (2 * (size_t)k + (w.run_begin(k) < d.item_at ? 1 : 0)) * SLOT + lane, 32);
-    attn_merge<C>(acc, merge, wn, lane);
-    if (wn == 0) attn_write<C>(a, acc, d.s, d.item, lane);
+    attn_merge<C>(acc, merge + which * (warps / 2) * SLOT, me, warps, lane);
+    if (me == 0) attn_write<C>(a, acc, d.s, d.item, lane);
   }
 }
 
