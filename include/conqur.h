@@ -608,11 +608,12 @@ int conqur_kv_status(void* cuda_stream);
  * whose bit is set in its mask (a tree: itself and its ancestors); mask_dev NULL: j <= i (a chain; T_b = 1 is ordinary decoding).
  * Query head h reads key head h / group:
  *   s_l = scale q . k_l over the positions seen,  out = softmax(s) V,  lse = ln sum exp(s)     (nothing seen: out = 0, lse = -inf)
- * Arithmetic: products of bf16 values, exact in fp32 (4-bit codes enter as integers), sums, maxima and exponentials in fp32; a probability enters the
- * product with the values rounded to bf16.  The sums over positions are split over the GPU in a way that depends on
+ * Arithmetic: products of bf16 values, exact in fp32 (4-bit codes enter as integers), sums, maxima and exponentials in fp32; a probability (bits 4: times its
+ * token's value step) enters the product with the values rounded to bf16.  bits 4: |q| < 2^31 and value steps < 2^28 (beyond, infinities appear).  The sums over positions are split over the GPU in a way that depends on
  * the lengths of all sequences of the call: the same call gives the same bits, another batch around a sequence may change last bits.
  * A page index outside the cache or a position outside the table is not seen and latches CONQUR_ERR_BAD_INDEX (as do a negative context,
  * more than max_nodes drafted tokens, and rows outside q).  Values that are not finite reach the rows that see them only.
+ * CONQUR_ERR_TIMEOUT is latched, and rows may be missing, when a wait inside the kernel ran out (about 2 s).
  */
 typedef struct {
   uint32_t struct_size;     /* = sizeof(conqur_tree_call) */

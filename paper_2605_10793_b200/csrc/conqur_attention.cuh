@@ -3,8 +3,9 @@
 //
 //   s_l = scale q . k_l,  o = sum_l 2^(s_l log2 e - m) v_l / sum_l 2^(s_l log2 e - m),  m a running bound of the row's scores
 //
-// What bounds it: the cache is read once and every byte of it meets at most a few hundred rows, so with few rows memory sets the
-// pace, with a tree of some dozen rows the unpacking and the products do.
+// This file: at most 16 rows a key head.  The cache is read once, so memory sets the pace; over 4-bit codes the unpacking of a byte into two operands comes
+// close to it.  Measured on one row of 8 key heads of 4 query heads each, 64 sequences of 8192: bf16 322 us (6.67 TB/s, a copy's rate), 4 bits 124 us (4.6 TB/s:
+// about 1.1 instructions a code at two thirds of the issue rate); one sequence of 200: 9 us, of which 3 are a launch.
 //   - The tokens, not the rows, are the 16-row side of the warps' products (m16n8k16): S^T = K Q^T and O^T = V^T P^T.  Eight
 //     rows fill an instruction, and a fragment of K or V that was unpacked from codes is used for all rows of the warp.  The codes go from shared memory to the
 //     fragments in registers, in an order of dimensions (and of output dimensions) that lets every lane read whole words of a token's row;
@@ -13,7 +14,7 @@
 //   - The running maximum is only a bound: rows are rescaled when a score exceeds it by 2^8, one vote per 16 tokens instead of a
 //     reduction (P is rounded relatively, a common factor changes nothing).
 //   - The work, in tiles of tokens of one sequence, key head and block of rows, is laid end to end and cut into equal runs, one per
-//     resident CTA, whatever the lengths.  A piece of work that is cut leaves its parts (accumulators, maximum, sum) in the workspace; the
+//     resident CTA, whatever the lengths (Walk has the exception for few items).  A piece of work that is cut leaves its parts (accumulators, maximum, sum) in the workspace; the
 //     last CTA to finish one of its parts adds them up in their order.  No CTA waits for another.
 //   - A warp takes groups of 32 tokens of its own and brings them with asynchronous 16-byte copies into a ring of its own: no warp waits for another
 //     but the one that adds up an item's parts: the warps take turns at that, the others go on with the next item.
@@ -45,7 +46,8 @@ constexpr int ATTN_UNIT = 64;                                    // tokens: what
 
 constexpr int ATTN_CHUNK = 32;                                   // tokens a warp takes at a time: each half lies in one page
 
-// BITS of the cache, D; a block works on 8 NT query rows with WN warps, each with a ring of STAGES chunks.
+// BITS of the cache, D; a block works on 8 NT query rows with WN warps, each with a ring of STAGES chunks.  MIN_RUN: tiles a CTA takes at least (one for each pair
+// of its warps: with 1, a sequence of 200 took 11.2 us, with 4 9.2).
 template <int BITS_, int D_, int NT_, int WN_, int STAGES_, int PER_SM_>
 struct AttnCfg {
   static constexpr int BITS = BITS_, D = D_, NT = NT_, WN = WN_, STAGES = STAGES_, PER_SM = PER_SM_;
@@ -54,14 +56,13 @@ struct AttnCfg {
   static constexpr int ROWS = 8 * NT;                            // query rows of a block
   static constexpr int STAGE_BYTES = ATTN_CHUNK * (BITS == 4 ? D + 8 : 4 * D);
   static constexpr int KS = D / 16;                              // k steps of the first product, 16-dimension tiles of the second
-  static constexpr int HALVES = NT <= 2 ? 2 : 1;                 // groups of 16 tokens that go through the computation together
-  static constexpr bool QREGS = NT <= 2 && PER_SM < 3;           // the rows' fragments stay in registers
   static constexpr int ACC = NT * KS * 4;                        // accumulators a lane
   static constexpr int PART = ACC + 6 * NT;                      // and its maxima, sums and sums of p z
   static constexpr int MERGE_BYTES = (WN - 1) * PART * 32 * 4;
   static constexpr int AUX_BYTES = 1024;
   static constexpr int SMEM = WN * STAGES * STAGE_BYTES + MERGE_BYTES + AUX_BYTES;
   static_assert((SMEM + 1024) * PER_SM <= 228 * 1024, "shared memory of an SM");
+  static_assert(NT <= 2, "the rows' fragments and sums stay in registers");
   static_assert(STAGES <= 16 && (WN & (WN - 1)) == 0, "two bits for every stage; the warps' parts are added in halves");
 };
 
@@ -474,7 +475,7 @@ __device__ __forceinline__ void attn_merge(Acc<C>& acc, float* buf, int me, int 
 template <typename C>
 struct Query {
   const __nv_bfloat16* p[C::NT];     // NULL: no such row
-  uint2 f[C::QREGS ? C::KS : 1][C::QREGS ? C::NT : 1];
+  uint2 f[C::KS][C::NT];
   float sum[C::NT][2];               // 4 bits: sums of rows 2 (lane & 3) and + 1, in the units of the products
   int first, rows;                   // the block's first row; rows of the sequence
 
@@ -493,9 +494,6 @@ struct Query {
   static __device__ __forceinline__ uint2 scaled(uint2 v) {
     // even nibbles meet the first two of four dimensions with 2^96, odd ones the others with 2^92
     return C::BITS == 4 ? make_uint2(mul2(v.x, 0x6F806F80u), mul2(v.y, 0x6D806D80u)) : v;
-  }
-  __device__ __forceinline__ uint2 get(int k, int n, int c) const {
-    return C::QREGS ? f[C::QREGS ? k : 0][C::QREGS ? n : 0] : scaled(load(k, n, c));
   }
   __device__ __forceinline__ void begin(const AttnArgs& a, const Seq& s, int item, int lane) {
     const int g = lane >> 2, c = lane & 3;
@@ -517,7 +515,7 @@ struct Query {
           const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x)), y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
           part += (x.x + x.y) + (y.x + y.y);
         }
-        if (C::QREGS) f[C::QREGS ? k : 0][C::QREGS ? n : 0] = scaled(v);
+        f[k][n] = scaled(v);
       }
       if (C::BITS == 4) {
         part += __shfl_xor_sync(0xffffffffu, part, 1);
@@ -538,13 +536,13 @@ struct Query {
   }
 };
 
-// A chunk against the rows: HALVES times 16 tokens, from `at` on.  `pos`: the first one's position in the sequence; `bad`: halves that could not be read.
+// A chunk of twice 16 tokens against the rows.  `pos`: the first one's position in the sequence; `bad`: halves that could not be read.
 // EDGE: some position is not seen by some row (drafted tokens, the end of the sequence, a page that could not be read).  Both halves go through
 // each stage of the computation together: what one waits for (products, exponentials) the other fills.
 template <typename C, bool EDGE>
-__device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint32_t stage, int at, int pos, const Seq& s, uint32_t bad,
+__device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint32_t stage, int pos, const Seq& s, uint32_t bad,
                                             const Query<C>& query, int lane) {
-  constexpr int H = C::HALVES;
+  constexpr int H = 2;
   const int g = lane >> 2, c = lane & 3;
   constexpr int D = C::D, KS = C::KS, NT = C::NT, CT = ATTN_CHUNK;
   float sc[H][NT][4], ks[H][2];
@@ -552,7 +550,7 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
   // ---- S^T = K Q^T: rows (tokens) g and g + 8, columns (query rows) 2c and 2c + 1
 #pragma unroll
   for (int u = 0; u < H; ++u) {
-    const int au = at + 16 * u;
+    const int au = 16 * u;
     float sd[NT][4];                   // (the k steps alternate between two sums: a product that waits for the one before it takes several times its issue)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -581,7 +579,7 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
         const uint32_t f[4] = {codes_even(x0), codes_even(x1), codes_odd(x0), codes_odd(x1)};
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint2 q = query.get(k, n, c);
+          const uint2 q = query.f[k][n];
           mma16816((k & 1) ? sd[n] : sc[u][n], f, q.x, q.y);
         }
       }
@@ -603,7 +601,7 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
         ldmatrix4(f, stage + (uint32_t)((k >> 2) * CT + au + t) * 128 + ((piece ^ (t & 7)) << 4));
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint2 q = query.get(k, n, c);
+          const uint2 q = query.f[k][n];
           mma16816((k & 1) ? sd[n] : sc[u][n], f, q.x, q.y);
         }
       }
@@ -669,7 +667,7 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
   for (int u = 0; u < H; ++u) {
     float v0 = 1.f, v1 = 1.f;
     if (C::BITS == 4) {
-      const uint32_t vr = stage + CT * (D + 4) + (at + 16 * u) * 4 + g * 4;
+      const uint32_t vr = stage + CT * (D + 4) + (16 * u) * 4 + g * 4;
       v0 = step_of(lds32(vr)) * ATTN_P_UP;
       v1 = step_of(lds32(vr + 32)) * ATTN_P_UP;
     }
@@ -694,7 +692,7 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
   // ---- O^T += V^T P^T
 #pragma unroll
   for (int u = 0; u < H; ++u) {
-    const int au = at + 16 * u;
+    const int au = 16 * u;
     if (C::BITS == 4) {
       // the pairs of tokens (2c, 2c + 1) and (2c + 8, 2c + 9); dimensions g * D/8 ... of each
       const uint32_t vr = stage + CT * (D + 4) + au * 4 + 2 * c * 4;
@@ -872,11 +870,8 @@ __global__ void __launch_bounds__(C::THREADS, C::PER_SM) attn_kernel(const AttnA
       const uint32_t lost = first + 16 < end ? bad : bad & 1u;           // (a second half behind the end is not fetched)
       if (lost && lane == 0) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
       const bool edge = first + ATTN_CHUNK > w.s.context || lost;
-#pragma unroll 1
-      for (int at = 0; at < ATTN_CHUNK && first + at < end; at += 16 * C::HALVES) {
-        if (!edge) attn_tokens<C, false>(a, acc, stage, at, 0, w.s, 0u, query, lane);
-        else attn_tokens<C, true>(a, acc, stage, at, first + at, w.s, bad >> (at / 16), query, lane);
-      }
+      if (!edge) attn_tokens<C, false>(a, acc, stage, 0, w.s, 0u, query, lane);
+      else attn_tokens<C, true>(a, acc, stage, first, w.s, bad, query, lane);
       __syncwarp();
       fetch.issue(a, &aux->ahead[wn], wn, lane);               // into the stage that is free now
       st = st + 1 == C::STAGES ? 0 : st + 1;
