@@ -473,33 +473,32 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
             if (!(((j < 32 ? lo : hi) >> (j & 31)) & 1u)) s[j] = -INFINITY;
         };
         float s[64];
-        tmem_read64(tS, s);
-        const float neg = m == -INFINITY ? 3e38f : -m;         // (no bound yet: whatever is finite raises it)
-        const uint64_t neg2 = two(neg, neg);
-#pragma unroll
-        for (int j = 0; j < 64; j += 4) {
-          const ulonglong2 k = kstep(j);
-          const float2 x = apart(two_fma(two(s[j], s[j + 1]), k.x, neg2)), y = apart(two_fma(two(s[j + 2], s[j + 3]), k.y, neg2));
-          s[j] = x.x; s[j + 1] = x.y; s[j + 2] = y.x; s[j + 3] = y.y;
-        }
-        if (edge) blind(s);
-        float top = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 64; j += 2) top = fmaxf(top, fmaxf(s[j], s[j + 1]));
-        // a score above the bound by 2^8 (there is none yet: any) raises it
-        const bool raise = __any_sync(0xffffffffu, top > 8.f);
-        if (raise) {
+        auto against = [&](float neg) {                        // scores minus the bound; their maximum
+          const uint64_t neg2 = two(neg, neg);
           tmem_read64(tS, s);
-          top = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 64; j += 4) {
             const ulonglong2 k = kstep(j);
-            const float2 x = apart(two_mul(two(s[j], s[j + 1]), k.x)), y = apart(two_mul(two(s[j + 2], s[j + 3]), k.y));
+            const float2 x = apart(two_fma(two(s[j], s[j + 1]), k.x, neg2)), y = apart(two_fma(two(s[j + 2], s[j + 3]), k.y, neg2));
             s[j] = x.x; s[j + 1] = x.y; s[j + 2] = y.x; s[j + 3] = y.y;
           }
-          blind(s);
+          if (edge) blind(s);
+          float top = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 64; j += 2) top = fmaxf(top, fmaxf(s[j], s[j + 1]));
+          return top;
+        };
+        // A score above the bound by 2^8 (there is none yet: any) raises it: the row's own scores decide, whatever its neighbours in the warp do.
+        const bool up = against(m == -INFINITY ? 3e38f : -m) > 8.f;
+        const bool raise = __any_sync(0xffffffffu, up);
+        float f = 1.f;
+        if (raise) {
+          const float top = against(0.f);
+          if (up) {
+            f = ex2(m - top);
+            m = top;
+          }
+          against(m == -INFINITY ? 3e38f : -m);
         }
         ptx::tc_fence_before();
         ptx::mbar_arrive(&aux->read[buf]);
@@ -507,9 +506,6 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         if (!(ok = tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag))) break;
         ptx::tc_fence_after();
         if (raise) {
-          const bool up = top > m;                             // (rows below theirs are raised too: no harm)
-          const float f = up ? ex2(m - top) : 1.f;
-          if (up) m = top;
           l *= f;
           if (i > i0) {                                        // (the item's first tile overwrites O)
 #pragma unroll 1
@@ -522,9 +518,6 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
             }
             tmem_write_wait();
           }
-          const float bound = m == -INFINITY ? 0.f : m;
-#pragma unroll
-          for (int j = 0; j < 64; ++j) s[j] -= bound;          // (not seen: stays -inf)
         }
         uint64_t sum = two(0.f, 0.f);                          // a tile's probabilities by themselves: fewer roundings of a long sum
 #pragma unroll

@@ -463,6 +463,121 @@ def test_strided_queries_no_lse_streams_and_graphs():
     assert B.conqur_kv_status() == 0 and warm.shape == out.shape
 
 
+@pytest.mark.parametrize("bits", [4, 16])
+def test_more_rows_long_split_many_sequences_and_rising_scores(bits):
+    """More than 16 rows a key head: an item over many CTAs, the same bits again through one workspace; more sequences than a warp takes at a time, some
+    empty; scores whose maximum rises along the positions."""
+    B, torch = _B(), _t()
+    s = Setup(71, [20000], [20], 2, 4, 128, 64, bits)
+    ws = B.attention_workspace(s.cache, 4, 20)
+    out, lse = s.run(workspace=ws)
+    s.check(out, lse)
+    for _ in range(3):
+        o2, l2 = s.run(workspace=ws, out=torch.full_like(out, 7.0), lse=torch.full_like(lse, 7.0))
+        assert torch.equal(o2, out) and torch.equal(l2, lse)
+    rng = np.random.default_rng(72)
+    contexts, nodes = [int(x) for x in rng.integers(0, 200, 75)], [int(x) for x in rng.integers(0, 5, 75)]
+    contexts[50], nodes[50] = 3000, 4
+    m = Setup(73, contexts, nodes, 2, 6, 64, 16, bits)
+    m.check(*m.run(max_nodes=4))
+    u = Setup(74, [700, 130, 64], [9, 20, 3], 1, 4, 128, 32, bits, sharp=12.0)
+    u.check(*u.run())
+    assert B.conqur_kv_status() == 0
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_more_rows_values_that_are_not_finite_bad_pages_and_odd_queries(bits):
+    """More than 16 rows a key head: NaN and infinity in a drafted token's key or value, in a context token's value, in one query; pages that are not there."""
+    B, torch = _B(), _t()
+    nodes, group = 6, 8
+    for context in (0, 5, 130):
+        s = Setup(81, [context, 40], [nodes, 1], 1, group, 128, 16, bits)
+        masks = [1, 1 | 2, 1 | 4, 1 | 2 | 8, 16, 1 | 32]                       # token 1 is seen by tokens 1 and 3
+        s.masks[0] = masks
+        s.mask = torch.tensor(masks + [1, 0, 0], device="cuda")
+        clean, clse = (x.clone() for x in s.run())
+        s.check(clean, clse)
+        fresh = lambda: dict(out=torch.full_like(clean, 7.0), lse=torch.full_like(clse, 7.0))
+        for pos, hit in ((context + 1, [1, 3]), (context // 2, list(range(nodes)))):
+            if pos == context and context == 0:
+                continue
+            slot = s.dev["table"][0, pos // 16].long() * 16 + pos % 16
+            for which in ("k", "v"):
+                old = s.data.clone()
+                k, v = (_dev(x[0][pos:pos + 1]) for x in (s.k, s.v))
+                (k if which == "k" else v)[0, 0, 3] = float("nan")
+                (k if which == "k" else v)[0, 0, 77] = float("inf")
+                B.conqur_kv_append(s.cache, k, v, slot[None])
+                out, lse = s.run(**fresh())
+                s.data.copy_(old)
+                rest = [i for i in range(out.shape[0]) if i not in hit]
+                assert torch.equal(out[rest], clean[rest]) and torch.equal(lse[rest], clse[rest])
+                if which == "k" or bits == 4:
+                    assert torch.isnan(out[hit]).all()
+                else:
+                    assert torch.isnan(out[hit][..., 3]).all() and torch.isinf(out[hit][..., 77]).all()
+        # one query row
+        q = s.dev["q"].clone()
+        s.dev["q"][2, 5, 60] = float("nan")
+        out, lse = s.run(**fresh())
+        s.dev["q"] = q
+        assert torch.isnan(out[2, 5]).all() and torch.isnan(lse[2, 5])
+        out[2, 5], lse[2, 5] = clean[2, 5], clse[2, 5]
+        assert torch.equal(out, clean) and torch.equal(lse, clse)
+    assert B.conqur_kv_status() == 0
+    s.dev["table"][0, 3] = 10 ** 6                                             # positions 48 .. 63 of the first sequence
+    out, lse = s.run(**fresh())
+    assert B.conqur_kv_status() == -11 and torch.equal(out[nodes:], clean[nodes:])
+    seen = np.zeros((nodes, context + nodes), bool)
+    seen[:, :context] = True
+    for i in range(nodes):
+        for j in range(nodes):
+            seen[i, context + j] = (masks[i] >> j) & 1
+    seen[:, 48:64] = False
+    for h in range(group):
+        want, _, mass, size = K.attend(s.q[:nodes, h], s.k[0][:, 0], s.v[0][:, 0], seen, 128 ** -0.5)
+        bound = (2.0 ** -8 + 2.0 ** -17 * size[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want)
+        bound += _codes_bound(s.step[0][:, 0], s.k[0][:, 0], s.q[:nodes, h], seen, 128 ** -0.5)
+        assert (np.abs(out[:nodes, h].float().cpu().numpy() - want) <= bound).all()
+
+
+def test_more_rows_on_two_streams_and_in_a_graph():
+    """More than 16 rows a key head: two calls at once with workspaces of their own, and a captured call replayed with other lengths."""
+    B, torch = _B(), _t()
+    s = Setup(91, [900, 2500, 64], [8, 5, 8], 2, 4, 128, 32, 4)
+    good, glse = (x.clone() for x in s.run())
+    s.check(good, glse)
+    ws = [B.attention_workspace(s.cache, 4, 8) for _ in range(2)]
+    outs = [torch.full_like(good, 7.0) for _ in range(2)]
+    lses = [torch.full_like(glse, 7.0) for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        s.run(out=outs[0], lse=lses[0], workspace=ws[0])
+        with torch.cuda.stream(side):
+            s.run(out=outs[1], lse=lses[1], workspace=ws[1])
+    torch.cuda.current_stream().wait_stream(side)
+    for o, l in zip(outs, lses):
+        assert torch.equal(o, good) and torch.equal(l, glse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.run(out=outs[0], lse=lses[0], workspace=ws[0])
+    old = s.contexts
+    for cut in (0, 1, 63):
+        s.contexts = [c - cut for c in old]
+        s.dev["contexts"].copy_(torch.tensor(s.contexts, dtype=torch.int32))
+        # the drafted tokens are then those that lie behind the shorter context
+        outs[0].fill_(7.0)
+        lses[0].fill_(7.0)
+        graph.replay()
+        keep = [(k, v) for k, v in zip(s.k, s.v)], s.step
+        s.k, s.v = [k[: c + n] for k, c, n in zip(s.k, s.contexts, s.nodes)], [v[: c + n] for v, c, n in zip(s.v, s.contexts, s.nodes)]
+        s.step = [x[: c + n] for x, c, n in zip(s.step, s.contexts, s.nodes)]
+        s.check(outs[0], lses[0])
+        s.k, s.v, s.step = [x[0] for x in keep[0]], [x[1] for x in keep[0]], keep[1]
+    assert B.conqur_kv_status() == 0
+
+
 def test_cache_past_4_gigabytes():
     """Pages whose byte offset needs more than 32 bits, and slots past 2^22."""
     B, torch = _B(), _t()
