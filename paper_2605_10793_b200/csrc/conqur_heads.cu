@@ -312,28 +312,39 @@ __device__ __forceinline__ void token_of(const HeadsArgs& a, int64_t t, int64_t&
   }
 }
 
-// cos and sin of the lane's eight pairs (times the amplitude; the sine times `sign`); 1 and 0 where they do not turn.
-__device__ __forceinline__ void lane_angles(const HeadsArgs& a, int64_t b, int64_t t, const LanePlan& q, float sign, f2 (&c)[4], f2 (&s)[4]) {
-  float cf[8], sf[8];
+// cos and sin of the lane's eight pairs (times the amplitude; the sine times `sign`); 1 and 0 where they do not turn.  Lanes with the same place in their
+// rows need the same ones: each computes its share and they hand them round (the whole warp comes here).
+template <int D>
+__device__ __forceinline__ void lane_angles(const HeadsArgs& a, int64_t b, int64_t t, const LanePlan& q, int row, int l, float sign, f2 (&c)[4], f2 (&s)[4]) {
+  constexpr int L = Row<D>::L, PW = Row<D>::PER_WARP, E = (8 + PW - 1) / PW;
+  float cf[E], sf[E];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    cf[i] = 1.f;
-    sf[i] = 0.f;
+  for (int e = 0; e < E; ++e) {
+    cf[e] = 1.f;
+    sf[e] = 0.f;
   }
   if (q.turned) {
     const unsigned long long pos = (unsigned long long)a.pos[b * a.pos_b + t];
     const float amp = (float)__longlong_as_double((long long)a.table[a.rot >> 1]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (q.turned & (1u << i)) {
-        angle(pos, a.table[q.f[i >> 2] + (i & 3)], amp, cf[i], sf[i]);
-        sf[i] *= sign;
+    for (int e = 0; e < E; ++e) {
+      const int i = row * E + e;
+      if (i < 8 && ((q.turned >> i) & 1u)) {
+        angle(pos, a.table[(i < 4 ? q.f[0] : q.f[1]) + (i & 3)], amp, cf[e], sf[e]);
+        sf[e] *= sign;
       }
+    }
+  }
+  float cs[8], sn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    cs[i] = __shfl_sync(0xffffffffu, cf[i % E], (i / E) * L + l);
+    sn[i] = __shfl_sync(0xffffffffu, sf[i % E], (i / E) * L + l);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    c[i] = mk2(cf[2 * i], cf[2 * i + 1]);
-    s[i] = mk2(sf[2 * i], sf[2 * i + 1]);
+    c[i] = mk2(cs[2 * i], cs[2 * i + 1]);
+    s[i] = mk2(sn[2 * i], sn[2 * i + 1]);
   }
 }
 
@@ -379,7 +390,7 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 6 : 5) heads_k
         r[k][1].load(p + k * in_step + q.p1);
       }
     if (!have) {
-      lane_angles(a, b, t, q, a.inverse ? -1.f : 1.f, c, s);
+      lane_angles<D>(a, b, t, q, row, l, a.inverse ? -1.f : 1.f, c, s);
       have = true;
     }
     int k = 0;
@@ -476,7 +487,7 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 4 : 3) heads_g
     };
     if (h < heads) fetch();
     f2 c[4], s[4];
-    lane_angles(a, b, t, q, -1.f, c, s);
+    lane_angles<D>(a, b, t, q, row, l, -1.f, c, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       c[i] = mul2(c[i], mk2(scale));
