@@ -313,9 +313,9 @@ __device__ __forceinline__ void token_of(const HeadsArgs& a, int64_t t, int64_t&
 }
 
 // cos and sin of the lane's eight pairs (times the amplitude; the sine times `sign`); 1 and 0 where they do not turn.  Lanes with the same place in their
-// rows need the same ones: each computes its share and they hand them round (the whole warp comes here).
+// rows need the same ones: each computes its share and they hand them round (the whole warp comes here).  `pos` counts only where something turns.
 template <int D>
-__device__ __forceinline__ void lane_angles(const HeadsArgs& a, int64_t b, int64_t t, const LanePlan& q, int row, int l, float sign, f2 (&c)[4], f2 (&s)[4]) {
+__device__ __forceinline__ void lane_angles(const HeadsArgs& a, unsigned long long pos, const LanePlan& q, int row, int l, float sign, f2 (&c)[4], f2 (&s)[4]) {
   constexpr int L = Row<D>::L, PW = Row<D>::PER_WARP, E = (8 + PW - 1) / PW;
   float cf[E], sf[E];
 #pragma unroll
@@ -324,7 +324,6 @@ __device__ __forceinline__ void lane_angles(const HeadsArgs& a, int64_t b, int64
     sf[e] = 0.f;
   }
   if (q.turned) {
-    const unsigned long long pos = (unsigned long long)a.pos[b * a.pos_b + t];
     const float amp = (float)__longlong_as_double((long long)a.table[a.rot >> 1]);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -390,7 +389,7 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 6 : 5) heads_k
         r[k][1].load(p + k * in_step + q.p1);
       }
     if (!have) {
-      lane_angles<D>(a, b, t, q, row, l, a.inverse ? -1.f : 1.f, c, s);
+      lane_angles<D>(a, a.rot ? (unsigned long long)a.pos[b * a.pos_b + t] : 0ull, q, row, l, a.inverse ? -1.f : 1.f, c, s);
       have = true;
     }
     int k = 0;
@@ -470,24 +469,36 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 4 : 3) heads_g
   for (int i = 0; i < 4; ++i) dw.a[i] = dw.b[i] = 0ull;
   for (int e = threadIdx.x; e < D; e += HEADS_THREADS) weight[e] = load_weight(g.weight, a.weight_bf16, e);
   __syncthreads();
-  for (int64_t token = (int64_t)blk * HEADS_WARPS + warp; token < a.n; token += (int64_t)blocks * HEADS_WARPS) {
+  // position and first rows of the next token travel while the present one is worked on
+  const int64_t stride = (int64_t)blocks * HEADS_WARPS;
+  int64_t token = (int64_t)blk * HEADS_WARPS + warp;
+  const int heads = row < PW ? g.heads : 0;
+  const T *xp = nullptr, *yp = nullptr;
+  T* next_out = nullptr;
+  unsigned long long pos = 0ull;
+  Piece<T> x0, x1, y0, y1;
+  int h = row;
+  auto fetch = [&]() {
+    x0.load(xp + q.p0);
+    x1.load(xp + q.p1);
+    y0.load(yp + q.p0);
+    y1.load(yp + q.p1);
+  };
+  auto begin = [&](int64_t next) {
     int64_t b, t;
-    token_of(a, token, b, t);
-    const T* xp = static_cast<const T*>(g.in) + b * g.in_b + t * g.in_t + row * g.in_h;
-    const T* yp = static_cast<const T*>(g.grad) + b * g.grad_b + t * g.grad_t + row * g.grad_h;
-    T* op = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + row * g.out_h;
-    Piece<T> x0, x1, y0, y1;
-    int h = row;
-    const int heads = row < PW ? g.heads : 0;
-    auto fetch = [&]() {
-      x0.load(xp + q.p0);
-      x1.load(xp + q.p1);
-      y0.load(yp + q.p0);
-      y1.load(yp + q.p1);
-    };
+    token_of(a, next, b, t);
+    xp = static_cast<const T*>(g.in) + b * g.in_b + t * g.in_t + row * g.in_h;
+    yp = static_cast<const T*>(g.grad) + b * g.grad_b + t * g.grad_t + row * g.grad_h;
+    next_out = static_cast<T*>(g.out) + b * g.out_b + t * g.out_t + row * g.out_h;
+    if (a.rot) pos = (unsigned long long)a.pos[b * a.pos_b + t];
+    h = row;
     if (h < heads) fetch();
+  };
+  if (token < a.n) begin(token);
+  for (; token < a.n; token += stride) {
+    T* op = next_out;
     f2 c[4], s[4];
-    lane_angles<D>(a, b, t, q, row, l, -1.f, c, s);
+    lane_angles<D>(a, pos, q, row, l, -1.f, c, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       c[i] = mul2(c[i], mk2(scale));
@@ -504,7 +515,11 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 4 : 3) heads_g
       h += PW;
       xp += PW * g.in_h;
       yp += PW * g.grad_h;
-      if (h < heads) fetch();
+      if (it + 1 < total) {
+        if (h < heads) fetch();
+      } else if (token + stride < a.n) {
+        begin(token + stride);
+      }
       if (a.hadamard) row_hadamard<L>(y, l);
       row_spin<HALF>(y, c, s, q.turned);
       Piece<float> w0, w1;                                     // (shared memory: sixteen registers less)
