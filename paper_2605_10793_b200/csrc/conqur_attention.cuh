@@ -46,8 +46,8 @@ constexpr int ATTN_UNIT = 64;                                    // tokens: what
 
 constexpr int ATTN_CHUNK = 32;                                   // tokens a warp takes at a time: each half lies in one page
 
-// BITS of the cache, D; a block works on 8 NT query rows with WN warps, each with a ring of STAGES chunks.  MIN_RUN: tiles a CTA takes at least (one for each pair
-// of its warps: with 1, a sequence of 200 took 11.2 us, with 4 9.2).
+// BITS of the cache, D; a block works on 8 NT query rows with WN warps, each with a ring of STAGES chunks.  MIN_RUN: tiles a CTA takes at least, one for each pair
+// of its warps (one sequence of 200 over 4 bits: with 1 11.2 us, with 4 8.7; eight are better for some short batches, worse by as much for others).
 template <int BITS_, int D_, int NT_, int WN_, int STAGES_, int PER_SM_>
 struct AttnCfg {
   static constexpr int BITS = BITS_, D = D_, NT = NT_, WN = WN_, STAGES = STAGES_, PER_SM = PER_SM_;
@@ -188,9 +188,9 @@ struct Walk {
     const int grid = (int)gridDim.x;
     ctas = (int)min((long long)grid, (total + C::MIN_RUN - 1) / C::MIN_RUN);
     pad = 1;
-    if (items > 0 && items <= ctas) {
+    if (items > 0 && items <= grid) {
       // Runs that end with their item, if the grid has enough for it with up to four tiles more each than it would take otherwise: a run over two items
-      // costs its CTA about 6 us, four tiles 2.  (One sequence of 8192, 8 key heads: 22.5 to 16.0 us over 4 bits, 22.7 to 17.4 over bf16.)
+      // costs its CTA about 6 us, four tiles 2; and no item is cut that needs no cutting.  (One sequence of 8192, 8 key heads: 22.5 to 16.0 us over 4 bits, 22.7 to 17.4 over bf16.)
       constexpr int TRY = 2;
       const int run = max(C::MIN_RUN, (int)ratio(total + grid - 1, grid));
       int pieces[TRY] = {};
