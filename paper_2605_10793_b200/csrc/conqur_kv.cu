@@ -4,6 +4,8 @@
 // Writing and reading move every byte once and are bound by memory.  A row of head_dim elements lies in head_dim / 8 lanes, 16 bytes (bf16) each;
 // a lane's eight elements make one 32-bit word of codes.  Key and value row of a (token, head) are worked on together, two of them a lane, so that
 // 64 bytes a lane are in flight.
+// Measured, 32768 tokens of 8 heads of 128 into 4-bit codes and back: 69 us (51.7 at memory's rate); writing takes 39 of them under a profiler, where it issues 3.2 of 4
+// instructions a cycle.  With each lane dividing for itself and codes one by one: 87 us.
 // Codes are the ones that exact arithmetic gives: the step is rounded to bf16 BEFORE it divides, so y / step is a quotient of two 8-bit significands.
 // Such a quotient is a tie (k + 1/2) or at least 2^-9 away from one; y * (1 / step) in fp32 is off by 2^-19 at most, so rounding it to a
 // multiple of 2^-11 first restores the ties and disturbs nothing else, and no division per element is needed.
