@@ -43,7 +43,7 @@ EXPORTS = [
     "conqur_rope_frequencies", "conqur_rope_table_bytes", "conqur_rope_table", "conqur_rope_heads", "conqur_norm_rope_heads",
     "conqur_norm_rope_backward_scratch_bytes", "conqur_norm_rope_heads_backward",
     "conqur_kv_cache_bytes", "conqur_kv_append", "conqur_kv_read", "conqur_kv_status",
-    "conqur_tree_attention_workspace_bytes", "conqur_tree_attention",
+    "conqur_tree_attention_workspace_bytes", "conqur_tree_attention", "conqur_debug_tree_attention",
     "conqur_strerror",
 ]
 
@@ -209,6 +209,8 @@ def load() -> C.CDLL:
     lib.conqur_tree_attention_workspace_bytes.argtypes = [vp, i32, i32]
     lib.conqur_tree_attention.restype = C.c_int
     lib.conqur_tree_attention.argtypes = [vp, C.c_char_p, vp]
+    lib.conqur_debug_tree_attention.restype = C.c_int
+    lib.conqur_debug_tree_attention.argtypes = [vp, C.c_char_p, i32, i32, i32, vp]
     lib.conqur_strerror.restype = C.c_char_p
     lib.conqur_strerror.argtypes = [C.c_int]
     _lib = lib

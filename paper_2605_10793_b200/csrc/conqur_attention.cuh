@@ -38,6 +38,9 @@ struct AttnArgs {
   unsigned* counters;                // one per CTA, for the item that its run ends in the middle of: parts finished, wraps to 0
   float* parts;                      // two slots per CTA
   int* flags;
+  // conqur_attention_tc.cuh: cycles that a wait between the warps lasts at most, and (test support) the one wait that waits for what never comes
+  long long wait_limit;
+  int lose_block, lose_site, lose_tile;
 };
 
 enum { KV_FLAG_BAD_INDEX = 1, KV_FLAG_TIMEOUT = 2 };

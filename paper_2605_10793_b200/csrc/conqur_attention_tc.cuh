@@ -39,6 +39,7 @@ struct TreeCfg {
 template <typename C>
 struct TreeAux {
   uint64_t full[C::STAGES], empty[C::STAGES], scored[2], read[2], ready[2], done[2];   // tile brought, free again; S complete, read; P written; P V complete
+  uint64_t drained, never;                                     // all products of the CTA complete; test support: nothing arrives here
   float kstep[C::STAGES][64], vstep[C::STAGES][64];
   uint32_t bad[C::STAGES][2];                                  // tokens of a tile whose page could not be read
   float bound[2][128], sum[2][128];                            // of the two streams
@@ -143,6 +144,16 @@ __device__ __forceinline__ uint4 codes8(uint32_t w, uint32_t bias) {
 }
 __device__ __forceinline__ uint32_t zero_bias(uint32_t rec) { return fma_bf16x2(zero_of(rec) * 0x10001u, 0xFF00FF00u, 0x80008000u); }   // -z / 64
 __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+
+// The bounded wait of a whole warp; `site` (CONQUR_TREE_WAIT_*) and the tile's number in the CTA name it.
+template <typename C>
+__device__ __forceinline__ bool tree_wait(const AttnArgs& a, TreeAux<C>* aux, int site, int tile, uint64_t* bar, uint32_t parity) {
+  if (tile == a.lose_tile && site == a.lose_site && (int)blockIdx.x == a.lose_block) {
+    bar = &aux->never;
+    parity = 0u;
+  }
+  return __all_sync(0xffffffffu, tc_wait(bar, parity, &aux->abort_flag, a.wait_limit));
+}
 
 // ---- warps 8-11: a thread takes a token's 64 dimensions of one plane, of keys and values (D = 64: threads 0-63 the keys, 64-127 the values)
 template <typename C>
@@ -313,6 +324,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
   volatile int* abort_flag = &aux->abort_flag;
   const uint32_t tmem = aux->tmem, tO = tmem + C::T_O, tQ = tmem + C::T_Q, tP = tmem + C::T_P;
   Walk<C> w = aux->w;
+  bool issued = false;                                         // products: there are some that `drained` has to be asked about
   int cnt = 0;                                                 // tiles so far: stream and buffers cnt & 1, phase (cnt >> 1) & 1; stage cnt % S
   bool head_of_run = true, more = w.left > 0;
 
@@ -366,7 +378,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       int slot = 0;
       for (int i = i0; i < tiles; i += 2) {
         const int n = cnt + i, st = n % S;
-        if (!tc_wait_warp(&aux->empty[st], ((uint32_t)(n / S) & 1u) ^ 1u, abort_flag)) break;
+        if (!tree_wait<C>(a, aux, CONQUR_TREE_WAIT_STAGE, n, &aux->empty[st], ((uint32_t)(n / S) & 1u) ^ 1u)) break;
         uint8_t* mem = sT + st * STAGE;
         if (C::BITS == 16) {
           in.now[0] = in.next[0];
@@ -411,13 +423,14 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       const uint32_t t0 = ptx::smem_u32(sT);
       auto scores = [&](int n) {
         const int st = n % S;
-        if (!tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag)) return false;
+        if (!tree_wait<C>(a, aux, CONQUR_TREE_WAIT_TILE, n, &aux->full[st], (uint32_t)(n / S) & 1u)) return false;
         ptx::tc_fence_after();
         const uint32_t k0 = t0 + st * STAGE;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
           umma_from_tmem(leader, tmem + (n & 1) * 64, tQ + j * 8, tc_smem_desc(k0 + (j >> 2) * 8192 + (j & 3) * 32, 16, 1024), id_s, j > 0 ? 1u : 0u);
         ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->scored[n & 1]));
+        issued = true;
         return true;
       };
       bool ok = scores(cnt) && (tiles < 2 || scores(cnt + 1));
@@ -431,13 +444,13 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
             ptx::tc_fence_after();
             if (!(ok = scores(n + 2))) break;
             next = true;
-          } else if (__any_sync(0xffffffffu, *abort_flag || clock64() - since > TC_WAIT_LIMIT)) {
+          } else if (__any_sync(0xffffffffu, *abort_flag || clock64() - since > a.wait_limit)) {
             *abort_flag = 1;
             ok = false;
             break;
           }
         }
-        if (!(ok = ok && tc_wait_warp(&aux->ready[buf], (n >> 1) & 1, abort_flag))) break;
+        if (!(ok = ok && tree_wait<C>(a, aux, CONQUR_TREE_WAIT_PROBABILITIES, n, &aux->ready[buf], (n >> 1) & 1))) break;
         ptx::tc_fence_after();
         const uint32_t v0 = t0 + (n % S) * STAGE + C::T_BYTES;
 #pragma unroll
@@ -458,7 +471,9 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       for (int i = i0; i < tiles; i += 2) {
         const int n = cnt + i, st = n % S, first = (w.tile + i) * ATTN_UNIT;
         // (the steps come with the tile, the scores with its product)
-        if (!(ok = tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag) && tc_wait_warp(&aux->scored[buf], (n >> 1) & 1, abort_flag))) break;
+        if (!(ok = tree_wait<C>(a, aux, 0, n, &aux->full[st], (uint32_t)(n / S) & 1u) &&
+                   tree_wait<C>(a, aux, CONQUR_TREE_WAIT_SCORES, n, &aux->scored[buf], (n >> 1) & 1)))
+          break;
         ptx::tc_fence_after();
         const uint32_t tS = tmem + lanes + buf * 64;
         const unsigned long long bad = (unsigned long long)aux->bad[st][0] | ((unsigned long long)aux->bad[st][1] << 32);
@@ -503,7 +518,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         ptx::tc_fence_before();
         ptx::mbar_arrive(&aux->read[buf]);
         // P and O of the stream's tile before
-        if (!(ok = tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag))) break;
+        if (!(ok = tree_wait<C>(a, aux, 0, n, &aux->done[buf], ((n >> 1) & 1) ^ 1))) break;
         ptx::tc_fence_after();
         if (raise) {
           l *= f;
@@ -546,7 +561,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         ptx::mbar_arrive(&aux->ready[buf]);
       }
       const int mine = tiles > i0 ? (tiles - 1 - i0) / 2 : -1, last = cnt + i0 + 2 * mine;      // the stream's last tile of the item
-      if (ok && mine >= 0) ok = tc_wait_warp(&aux->done[buf], (last >> 1) & 1, abort_flag);
+      if (ok && mine >= 0) ok = tree_wait<C>(a, aux, CONQUR_TREE_WAIT_OUTPUT, last, &aux->done[buf], (last >> 1) & 1);
       ptx::tc_fence_after();
       aux->bound[buf][r] = m;
       aux->sum[buf][r] = l;
@@ -686,6 +701,13 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
     head_of_run = false;
     more = w.next(a);
   }
+  if (ROLE == TREE_PRODUCTS && issued) {
+    // A wait that ran out leaves products under way: they end before TMEM, the tiles and the barriers they arrive on are given back.
+    ptx::umma_commit_by<false>(ptx::elect_one(), ptx::smem_u32(&aux->drained));
+    const long long since = clock64();
+    while (!arrived(&aux->drained, 0u))
+      if (__any_sync(0xffffffffu, clock64() - since > TC_WAIT_LIMIT)) break;
+  }
 }
 
 template <typename C>
@@ -710,6 +732,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
       ptx::mbar_init(&aux->ready[i], 128);
       ptx::mbar_init(&aux->done[i], 1);
     }
+    ptx::mbar_init(&aux->drained, 1);
+    ptx::mbar_init(&aux->never, 1);
     aux->abort_flag = aux->odd = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async();
@@ -738,9 +762,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 16) tree_role<C, TREE_PRODUCTS>(a, aux, sT, sRaw, warp);
   }
-  if (tid == 0 && *abort_flag) atomicOr(a.flags, KV_FLAG_TIMEOUT);
   ptx::tc_fence_before();
   __syncthreads();
+  if (tid == 0 && *abort_flag) atomicOr(a.flags, KV_FLAG_TIMEOUT);       // (behind the barrier: whichever warp gave up, and however late)
   if (warp == 16) ptx::tmem_dealloc(aux->tmem, 512);
 }
 

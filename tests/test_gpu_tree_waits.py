@@ -1,0 +1,54 @@
+"""Waits of the attention for more than 16 rows a key head that run out: the call ends, tells of it and leaves the process usable."""
+import pytest
+
+from tests.test_gpu_kv_cache import Setup, _B, _t
+
+pytestmark = pytest.mark.gpu
+
+STAGE, TILE, PROBABILITIES, SCORES, OUTPUT = 1, 2, 3, 4, 5
+TIMEOUT = -8
+
+
+def _lose(s, ws, out, lse, block, site, tile):
+    B, torch = _B(), _t()
+    d, heads = s.d, s.hk * s.group
+    call = B._TREE_CALL.pack(B._TREE_CALL.size, len(s.nodes), s.group, max(s.nodes), d ** -0.5, s.dev["table"].shape[1], s.rows, s.dev["q"].data_ptr(), heads * d, d,
+                             out.data_ptr(), heads * d, d, lse.data_ptr(), heads, s.dev["starts"].data_ptr(), s.dev["contexts"].data_ptr(),
+                             s.dev["table"].data_ptr(), s.dev["table"].stride(0), s.mask.data_ptr(), ws.data_ptr(), ws.numel())
+    return B.load().conqur_debug_tree_attention(s.cache._ref, call, block, site, tile, torch.cuda.current_stream().cuda_stream)
+
+
+def _fresh(s):
+    torch = _t()
+    return torch.full_like(s.out, 7.0), torch.full_like(s.lse, 7.0)
+
+
+# Three sequences of 15, 40 and 2 tiles and two key heads: runs of four tiles, one item each, so 4 + 4, 10 + 10 and 1 + 1 blocks, the last two with a whole item.
+LOST = [(0, STAGE, 1), (0, STAGE, 3), (0, TILE, 0), (0, TILE, 2), (3, PROBABILITIES, 0), (3, PROBABILITIES, 2), (9, SCORES, 0), (9, SCORES, 3),
+        (0, OUTPUT, 2), (0, OUTPUT, 3), (28, OUTPUT, 0), (28, OUTPUT, 1), (28, SCORES, 1), (28, PROBABILITIES, 0)]
+
+
+def _setup(bits, d):
+    s = Setup(91, [900, 2500, 64], [8, 5, 8], 2, 4, d, 32, bits)
+    s.run()
+    assert _B().conqur_kv_status() == 0
+    return s, s.out.clone(), s.lse.clone()
+
+
+@pytest.mark.parametrize("bits,d", [(4, 128), (16, 128), (4, 64), (16, 64)])
+def test_lost_waits_end_the_call_and_are_told_of(bits, d):
+    """Whichever warp gives up and whatever is under way then: the kernel ends, the status says so once, and with a zeroed workspace the next call is right."""
+    B, torch = _B(), _t()
+    s, good, glse = _setup(bits, d)
+    ws = B.attention_workspace(s.cache, 4, 8)
+    for block, site, tile in LOST:
+        out, lse = _fresh(s)
+        assert _lose(s, ws, out, lse, block, site, tile) == 0
+        assert B.conqur_kv_status() == TIMEOUT and B.conqur_kv_status() == 0, (block, site, tile)
+        ws.zero_()
+        out, lse = s.run(out=out, lse=lse, workspace=ws)
+        assert torch.equal(out, good) and torch.equal(lse, glse) and B.conqur_kv_status() == 0, (block, site, tile)
+    # a wait that the run does not come to: an ordinary call
+    out, lse = _fresh(s)
+    assert _lose(s, ws, out, lse, 28, STAGE, 9) == 0 and B.conqur_kv_status() == 0
+    assert torch.equal(out, good) and torch.equal(lse, glse)
