@@ -613,7 +613,7 @@ int conqur_kv_status(void* cuda_stream);
  * the lengths of all sequences of the call: the same call gives the same bits, another batch around a sequence may change last bits.
  * A page index outside the cache or a position outside the table is not seen and latches CONQUR_ERR_BAD_INDEX (as do a negative context,
  * more than max_nodes drafted tokens, and rows outside q).  Values that are not finite reach the rows that see them only.
- * CONQUR_ERR_TIMEOUT is latched, and rows may be missing, when a wait inside the kernel ran out (about 2 s).
+ * CONQUR_ERR_TIMEOUT is latched when a wait inside the kernel ran out (about 2 s): rows may then be missing (left as they were); those written are right.
  */
 typedef struct {
   uint32_t struct_size;     /* = sizeof(conqur_tree_call) */

@@ -9,7 +9,8 @@
 //   warp 16          issues the products: the scores of a stream's next tile as soon as those of the present one are read
 // The bound of a row is raised only when a score exceeds it by 2^8; then its accumulators are read, scaled and written back.  Values that are not finite meet
 // zeros of rows that do not see them only among the drafted tokens; there they are left out of the product and added at the item's end.  Work is cut into runs and
-// parts are joined as in conqur_attention.cuh.  Every wait between the warps is bounded: when one runs out the CTA latches TIMEOUT, writes nothing more and ends.
+// parts are joined as in conqur_attention.cuh.  Every wait between the warps is bounded: when one runs out the CTA latches TIMEOUT,
+// leaves the item that it is at and all later ones unwritten, waits for its products under way and ends.
 // Floor: 8192 exponentials a tile at 16 a cycle are 512 cycles, and the products take as long.  Measured, 37 sequences of 6000, 8 key heads, 128 rows: 159 us over
 // 4 bits, about 1500 cycles a tile (a half-used issue rate: the chain score - exponential - product of two streams is what is left), 223 us over bf16 (two
 // thirds of it the cache's bytes).  Sixteen rows in the kernel of conqur_attention.cuh take 78 us there, 32 rows would take two passes of it: 155, and here 153.
@@ -47,7 +48,6 @@ struct TreeAux {
   uint32_t tmem;
   int abort_flag, last;
   int odd;                                                     // some value or step of a drafted token was not finite (never taken back: it only asks for a look)
-  int stop[2];                                                 // abort_flag as all warps of the rows and the products see it, at an item's start and end
 };
 
 // 32 lanes x 16 consecutive columns: thread t of the warp holds row (lane base + t).
@@ -145,6 +145,19 @@ __device__ __forceinline__ uint4 codes8(uint32_t w, uint32_t bias) {
 __device__ __forceinline__ uint32_t zero_bias(uint32_t rec) { return fma_bf16x2(zero_of(rec) * 0x10001u, 0xFF00FF00u, 0x80008000u); }   // -z / 64
 __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
+// A barrier that tells all of its threads whether any of them brought `mine`.
+__device__ __forceinline__ bool bar_any(int bar, int threads, bool mine) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %3, 0;\n\t"
+      "bar.red.or.pred q, %1, %2, p;\n\t"
+      "selp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"(bar), "r"(threads), "r"((uint32_t)mine)
+      : "memory");
+  return any != 0u;
+}
 // The bounded wait of a whole warp; `site` (CONQUR_TREE_WAIT_*) and the tile's number in the CTA name it.
 template <typename C>
 __device__ __forceinline__ bool tree_wait(const AttnArgs& a, TreeAux<C>* aux, int site, int tile, uint64_t* bar, uint32_t parity) {
@@ -343,17 +356,16 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         }
         tmem_write16(tQ + ((uint32_t)(warp * 32) << 16) + c, x);
       }
-      if (tid == 0) aux->stop[0] = *abort_flag;
       tmem_write_wait();
       ptx::tc_fence_before();
     }
     if constexpr (ROLE != TREE_BRING) {                        // (keys and values run ahead into the next item)
       bar_sync(BAR_ITEM, 288);
-      if (*reinterpret_cast<volatile int*>(&aux->stop[0])) break;
       ptx::tc_fence_after();
     }
     const int tiles = w.end - w.tile;
     const int len = w.s.context + w.s.nodes;
+    bool ok = true;                                            // no wait of this warp's has run out in this item
 
     if constexpr (ROLE == TREE_BRING) {
       // ------------------------------------------------------------ keys and values
@@ -433,7 +445,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         issued = true;
         return true;
       };
-      bool ok = scores(cnt) && (tiles < 2 || scores(cnt + 1));
+      ok = scores(cnt) && (tiles < 2 || scores(cnt + 1));
       for (int i = 0; ok && i < tiles; ++i) {
         const int n = cnt + i, buf = n & 1;
         // the stream's next scores or this tile's P V, whichever can go first (a stage may have to be freed by this tile before the next keys come)
@@ -466,7 +478,6 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       const TreeRow row = tree_row<C>(a, w.s, w.item, r);
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       float m = -INFINITY, l = 0.f;
-      bool ok = true;
       const int i0 = (cnt ^ buf) & 1;                          // the stream's first tile of this item
       for (int i = i0; i < tiles; i += 2) {
         const int n = cnt + i, st = n % S, first = (w.tile + i) * ATTN_UNIT;
@@ -565,9 +576,9 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       ptx::tc_fence_after();
       aux->bound[buf][r] = m;
       aux->sum[buf][r] = l;
-      if (tid == 0) aux->stop[1] = *abort_flag;
-      bar_sync(BAR_ALL, 256);
-      if (!*reinterpret_cast<volatile int*>(&aux->stop[1])) {
+      // the item is written only if every warp of both streams has seen its last product: each brings its own outcome to the barrier
+      ok = !bar_any(BAR_ALL, 256, !ok);
+      if (ok) {
         const bool whole = w.tile == 0 && w.end == w.s.tiles;
         // the two streams together; each group of warps takes half of the columns
         const float m0 = aux->bound[0][r], m1 = aux->bound[1][r];
@@ -693,7 +704,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       ptx::tc_fence_before();
     }
     if constexpr (ROLE != TREE_BRING) {
-      bar_sync(BAR_ITEM, 288);                                 // rows and accumulators may be replaced
+      if (bar_any(BAR_ITEM, 288, !ok)) break;                  // rows and accumulators may be replaced
     } else {
       if (__any_sync(0xffffffffu, *abort_flag)) break;
     }

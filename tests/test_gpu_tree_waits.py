@@ -52,3 +52,51 @@ def test_lost_waits_end_the_call_and_are_told_of(bits, d):
     out, lse = _fresh(s)
     assert _lose(s, ws, out, lse, 28, STAGE, 9) == 0 and B.conqur_kv_status() == 0
     assert torch.equal(out, good) and torch.equal(lse, glse)
+
+
+@pytest.mark.parametrize("bits,d", [(4, 128), (16, 128)])
+def test_rows_of_a_lost_wait_are_right_or_left_as_they_were(bits, d):
+    """However late the wait runs out, and in one stream only: a row of a head is what an untroubled call gives, or is not touched."""
+    B, torch = _B(), _t()
+    s, good, glse = _setup(bits, d)
+    ws = B.attention_workspace(s.cache, 4, 8)
+    for block, site, tile in LOST:
+        out, lse = _fresh(s)
+        ws.zero_()
+        assert _lose(s, ws, out, lse, block, site, tile) == 0 and B.conqur_kv_status() == TIMEOUT
+        right = (out == good).all(dim=-1) & (lse == glse)
+        kept = (out == 7.0).all(dim=-1) & (lse == 7.0)
+        assert (right | kept)[:21].all(), (block, site, tile)
+        # the query heads of the item that the block works on, of its sequence's rows, and no others
+        rows, heads = slice(0, 8), slice(0, 4)
+        if block >= 28:
+            rows = slice(13, 21)
+        elif block >= 8:
+            rows = slice(8, 13)
+        want = torch.zeros_like(kept)
+        want[rows, heads] = True
+        want[21:] = True                                     # (behind the last sequence)
+        assert torch.equal(kept, want), (block, site, tile)
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_items_before_the_lost_wait_are_written(bits):
+    """Runs over several items: those that a block has finished are there, the one it gives up at and its later ones are not."""
+    B, torch = _B(), _t()
+    n = 200                                                  # 400 items of one tile on 148 blocks: about three a block
+    s = Setup(92, [40] * n, [9] * n, 2, 2, 128, 16, bits)
+    s.run()
+    good, glse = s.out.clone(), s.lse.clone()
+    ws = B.attention_workspace(s.cache, 2, 9)
+    for tile in (0, 1, 2):
+        out, lse = _fresh(s)
+        ws.zero_()
+        assert _lose(s, ws, out, lse, 2, OUTPUT, tile) == 0 and B.conqur_kv_status() == TIMEOUT
+        right = (out == good).all(dim=-1) & (lse == glse)
+        kept = (out == 7.0).all(dim=-1) & (lse == 7.0)
+        lost = kept[: 9 * n].reshape(n, 9, 2, 2)
+        assert (right | kept).all() and torch.equal(lost.any(dim=1).any(dim=-1), lost.all(dim=1).all(dim=-1))
+        items = int(lost.any(dim=1).any(dim=-1).sum())
+        if tile == 0:
+            first = items
+        assert items == first - tile and first >= 3
