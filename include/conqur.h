@@ -598,7 +598,7 @@ int conqur_kv_append(const conqur_kv_cache* cache, const void* K_dev, int64_t k_
 int conqur_kv_read(const conqur_kv_cache* cache, const int64_t* slots_dev, int64_t n, void* K_out_dev, void* V_out_dev, int32_t out_dtype,
                    void* cuda_stream);
 /* Synchronises the stream and returns the condition that the cache and attention calls on this device have latched since the last
- * such call (CONQUR_ERR_BAD_INDEX, CONQUR_ERR_TIMEOUT) or CONQUR_OK; clears it. */
+ * such call or CONQUR_OK, and clears it.  Of two conditions CONQUR_ERR_TIMEOUT comes first, CONQUR_ERR_BAD_INDEX with the next call. */
 int conqur_kv_status(void* cuda_stream);
 
 /*

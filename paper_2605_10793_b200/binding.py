@@ -629,7 +629,8 @@ def conqur_kv_read(cache: KVCache, slots, dtype=None):
 
 def conqur_kv_status() -> int:
     """Synchronise the current stream; condition latched by cache and attention calls since the last such call (0 = ok, -11: an index
-    outside its buffer was left out; CONQUR_ERR_TIMEOUT: a wait in an attention kernel ran out, its workspace is to be zeroed)."""
+    outside its buffer was left out; -8: a wait in an attention kernel ran out, its workspace is to be zeroed).  Of both, -8 comes first and
+    -11 with the next call."""
     import torch
     return int(load().conqur_kv_status(torch.cuda.current_stream().cuda_stream))
 

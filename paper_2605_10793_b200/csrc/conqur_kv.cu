@@ -12,6 +12,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <mutex>
 
@@ -24,7 +25,8 @@ using bf16 = __nv_bfloat16;
 
 namespace {
 
-__device__ int g_kv_flags;
+constexpr int KV_ANSWERS = 64;
+__device__ int g_kv_flags[1 + KV_ANSWERS];   // the conditions latched on this device; answers of conqur_kv_status
 
 struct RowsArgs {
   uint8_t* cache;
@@ -259,6 +261,13 @@ __global__ void __launch_bounds__(ROWS_THREADS) kv_read_kernel(const RowsArgs a)
   }
 }
 
+// Takes one condition out of the flags: each is seen and cleared in one step, and the other one, or what another stream latches meanwhile, stays.
+__global__ void kv_status_kernel(int* flags, int* answer) {
+  int told = atomicAnd(flags, ~kv::KV_FLAG_TIMEOUT) & kv::KV_FLAG_TIMEOUT;
+  if (!told) told = atomicAnd(flags, ~kv::KV_FLAG_BAD_INDEX) & kv::KV_FLAG_BAD_INDEX;
+  *answer = told;
+}
+
 // ---------------------------------------------------------------------------------------------------- host
 
 bool cache_ok(const conqur_kv_cache* c) {
@@ -423,12 +432,16 @@ extern "C" int conqur_kv_read(const conqur_kv_cache* cache, const int64_t* slots
 }
 
 extern "C" int conqur_kv_status(void* cuda_stream) {
+  static std::atomic<unsigned> calls{0};                       // callers on several threads get their answers in words of their own
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   int* flags = flags_here();
-  int f = 0;
-  if (!flags || cudaMemcpyAsync(&f, flags, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) return CONQUR_ERR_CUDA;
-  if (f && (cudaMemsetAsync(flags, 0, sizeof(int), s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)) return CONQUR_ERR_CUDA;
-  return (f & kv::KV_FLAG_TIMEOUT) ? CONQUR_ERR_TIMEOUT : (f & kv::KV_FLAG_BAD_INDEX) ? CONQUR_ERR_BAD_INDEX : CONQUR_OK;
+  int told = 0;
+  if (!flags) return CONQUR_ERR_CUDA;
+  int* answer = flags + 1 + calls.fetch_add(1u) % KV_ANSWERS;
+  kv_status_kernel<<<1, 1, 0, s>>>(flags, answer);
+  if (cudaGetLastError() != cudaSuccess || cudaMemcpyAsync(&told, answer, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
+    return CONQUR_ERR_CUDA;
+  return told == kv::KV_FLAG_TIMEOUT ? CONQUR_ERR_TIMEOUT : told == kv::KV_FLAG_BAD_INDEX ? CONQUR_ERR_BAD_INDEX : CONQUR_OK;
 }
 
 extern "C" size_t conqur_tree_attention_workspace_bytes(const conqur_kv_cache* cache, int32_t group, int32_t max_nodes) {

@@ -100,3 +100,25 @@ def test_items_before_the_lost_wait_are_written(bits):
         if tile == 0:
             first = items
         assert items == first - tile and first >= 3
+
+
+def test_two_conditions_are_told_of_one_after_the_other():
+    """A time-out and a bad slot, the slot's from another stream and possibly while the status is read: neither is lost."""
+    B, torch = _B(), _t()
+    s, good, glse = _setup(4, 128)
+    ws = B.attention_workspace(s.cache, 4, 8)
+    k = torch.randn(1, 2, 128, device="cuda").bfloat16()
+    beyond = torch.tensor([10 ** 9], device="cuda")
+    side = torch.cuda.Stream()
+    for both_first in (True, False, False, False):
+        out, lse = _fresh(s)
+        ws.zero_()
+        assert _lose(s, ws, out, lse, 0, SCORES, 0) == 0
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            B.conqur_kv_append(s.cache, k, k, beyond)
+        if both_first:
+            side.synchronize()
+        assert B.conqur_kv_status() == TIMEOUT
+        side.synchronize()
+        assert B.conqur_kv_status() == -11 and B.conqur_kv_status() == 0
