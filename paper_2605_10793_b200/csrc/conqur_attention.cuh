@@ -149,11 +149,14 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
   if (n > a.max_nodes) { n = a.max_nodes; bad = true; }
   if (c < 0) { c = 0; bad = true; }
   if (c > 0x7fff0000) { c = 0x7fff0000; bad = true; }       // positions stay below 2^31
+  // Positions that have no place in the table are not seen: no work for them, whatever the context says (one tile for rows that see nothing).
+  const long long reach = (long long)a.table_width << a.log_page;
+  if (n > 0 && c + n > reach) bad = true;
   if (bad && blockIdx.x == 0 && threadIdx.x < 32) atomicOr(a.flags, KV_FLAG_BAD_INDEX);
   s.start = (int)s0;
   s.nodes = (int)n;
   s.context = c;
-  s.tiles = n > 0 ? (int)(((long long)c + n + ATTN_UNIT - 1) / ATTN_UNIT) : 0;
+  s.tiles = n > 0 ? max(1, (int)((min(c + n, reach) + ATTN_UNIT - 1) / ATTN_UNIT)) : 0;
   s.blocks = (int)((n * a.group + C::ROWS - 1) / C::ROWS);
   return s;
 }

@@ -1,0 +1,48 @@
+"""Attention over the cache at the limits of its arguments."""
+import time
+
+import numpy as np
+import pytest
+
+from oracle import kv_oracle as K
+from tests.test_gpu_kv_cache import Setup, _B, _codes_bound, _t
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+@pytest.mark.parametrize("hk,group", [(2, 2), (1, 4), (2, 16)])
+def test_a_context_beyond_its_table_sees_the_table_and_costs_no_more(hk, group, bits):
+    """Positions without a place in the table are not seen, however many the context claims: the work is that of the table (2^24 tiles took seconds)."""
+    B, torch = _B(), _t()
+    s = Setup(101, [204, 205, 12], [4, 3, 2], hk, group, 128, 16, bits)       # the first two fill their 13 pages, and so the table
+    good, glse = (x.clone() for x in s.run())
+    s.check(good, glse)
+    ws = B.attention_workspace(s.cache, group, 4)
+    for claim in (205, 300, 2 ** 30, 2 ** 31 - 1):
+        s.dev["contexts"][0] = claim
+        torch.cuda.synchronize()
+        begin = time.perf_counter()
+        out, lse = s.run(out=torch.full_like(good, 7.0), lse=torch.full_like(glse, 7.0), workspace=ws)
+        assert B.conqur_kv_status() == -11
+        assert time.perf_counter() - begin < 0.2
+        assert torch.equal(out[4:], good[4:]) and torch.equal(lse[4:], glse[4:])
+        # its drafted tokens lie at `claim` and behind: those past position 207 have no place; the others see by their masks
+        seen = np.zeros((4, 208), bool)
+        seen[:, :claim] = True
+        for i in range(4):
+            for j in range(4):
+                if claim + j < 208:
+                    seen[i, claim + j] = (s.masks[0][i] >> j) & 1
+        for h in range(hk * group):
+            kh = h // group
+            want, wl, mass, size = K.attend(s.q[:4, h], s.k[0][:, kh], s.v[0][:, kh], seen, 128 ** -0.5)
+            delta = 2.0 ** -18 * size
+            bound = (2.0 ** -8 + 2 * delta[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want) + 1e-30
+            bound += _codes_bound(s.step[0][:, kh], s.k[0][:, kh], s.q[:4, h], seen, 128 ** -0.5)
+            assert (np.abs(out[:4, h].float().cpu().numpy() - want) <= bound).all(), (claim, h)
+            assert (np.abs(lse[:4, h].cpu().numpy() - wl) <= delta + 2.0 ** -20 * np.abs(wl) + 2.0 ** -13).all()
+    # no table at all: nothing is seen
+    s.dev["table"] = s.dev["table"][:, :0]
+    out, lse = s.run(out=torch.full_like(good, 7.0), lse=torch.full_like(glse, 7.0), workspace=ws)
+    assert B.conqur_kv_status() == -11 and not out[:9].any() and torch.isneginf(lse[:9]).all() and (out[9:] == 7.0).all()
