@@ -612,14 +612,16 @@ int conqur_kv_status(void* cuda_stream);
  * token's value step) enters the product with the values rounded to bf16.  bits 4: |q| < 2^31 and value steps < 2^28 (beyond, infinities appear).  The sums over positions are split over the GPU in a way that depends on
  * the lengths of all sequences of the call: the same call gives the same bits, another batch around a sequence may change last bits.
  * A page index outside the cache or a position outside the table is not seen and latches CONQUR_ERR_BAD_INDEX (as do a negative context,
- * more than max_nodes drafted tokens, and rows outside q).  Values that are not finite reach the rows that see them only.
+ * more than max_nodes drafted tokens, and rows outside q).  Of a sequence with more than max_nodes drafted tokens those behind the first max_nodes get
+ * NaN in out and lse; a sequence with rows outside q is left out.  Values that are not finite reach the rows that see them only.
  * CONQUR_ERR_TIMEOUT is latched when a wait inside the kernel ran out (about 2 s): rows may then be missing (left as they were); those written are right.
  */
 typedef struct {
   uint32_t struct_size;     /* = sizeof(conqur_tree_call) */
   int32_t  batch;           /* sequences, 0 .. 65535 */
   int32_t  group;           /* query heads per key head, 1 .. 64 */
-  int32_t  max_nodes;       /* at least every T_b; 1 .. 64 */
+  int32_t  max_nodes;       /* at least every T_b; 1 .. 64.  group * max_nodes, not the tokens there are, decides which kernel works: up to 16 the one
+                               that is fast for few rows, else the tensor cores' with blocks of 128 rows */
   float    scale;           /* finite */
   int32_t  table_width;     /* pages per row of the table */
   int64_t  rows;            /* rows of q and out; those no sequence names are left as they were */

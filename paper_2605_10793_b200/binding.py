@@ -650,7 +650,8 @@ def conqur_tree_attention(q, cache: KVCache, starts, contexts, table, mask=None,
 
     q: bf16 (tokens, q_heads, head_dim), the tokens of sequence b in rows starts[b] .. starts[b+1].  starts (b + 1), contexts (b),
     table (b, pages a sequence): int32.  mask: int64 (tokens,), bit j of a token's: it sees drafted token j of its sequence; None: a
-    chain.  max_nodes: the most tokens a sequence has (at most 64).  scale: 1 / sqrt(head_dim) by default.  out, lse (fp32 (tokens, q_heads)):
+    chain.  max_nodes: the most tokens a sequence has (at most 64); those of a sequence behind its first max_nodes get NaN and conqur_kv_status tells
+    of it.  It also chooses the kernel (up to 16 rows max_nodes * q_heads / kv_heads, or more), so no larger than needed.  scale: 1 / sqrt(head_dim) by default.  out, lse (fp32 (tokens, q_heads)):
     given or made here; rows that no sequence names stay as they are.  workspace: from attention_workspace; made here if None."""
     stream = _here(q)
     t, dev = _torch, cache._device

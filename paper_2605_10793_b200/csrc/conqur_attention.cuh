@@ -138,15 +138,20 @@ struct Seq {
   int start, nodes, context;
   int tiles, blocks;                 // units of tokens, blocks of rows
 };
+// over (where asked for): set if the sequence has more than max_nodes tokens.
 template <typename C>
-__device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
+__device__ __forceinline__ Seq sequence(const AttnArgs& a, int b, bool* over = nullptr) {
   Seq s;
   const long long s0 = a.starts[b], s1 = a.starts[b + 1];
   long long n = s1 - s0;
   int c = a.contexts[b];
   bool bad = false;
   if (s0 < 0 || n < 0 || s1 > a.rows) { n = 0; bad = true; }
-  if (n > a.max_nodes) { n = a.max_nodes; bad = true; }
+  if (n > a.max_nodes) {
+    n = a.max_nodes;
+    bad = true;
+    if (over) *over = true;
+  }
   if (c < 0) { c = 0; bad = true; }
   if (c > 0x7fff0000) { c = 0x7fff0000; bad = true; }       // positions stay below 2^31
   // Positions that have no place in the table are not seen: no work for them, whatever the context says (one tile for rows that see nothing).
@@ -159,6 +164,22 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
   s.tiles = n > 0 ? max(1, (int)((min(c + n, reach) + ATTN_UNIT - 1) / ATTN_UNIT)) : 0;
   s.blocks = (int)((n * a.group + C::ROWS - 1) / C::ROWS);
   return s;
+}
+
+// Tokens behind the first max_nodes of their sequence get NaN, by one warp of every CTA (rare: the call was given too small a max_nodes).
+template <typename C>
+__device__ void blank_rows(const AttnArgs& a) {
+  const int lane = threadIdx.x & 31, heads = a.kv_heads * a.group;
+  const uint4 nan = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
+  for (int b = 0; b < a.batch; ++b) {
+    const long long s0 = a.starts[b], s1 = a.starts[b + 1];
+    if (s0 < 0 || s1 > a.rows) continue;
+    for (long long row = s0 + a.max_nodes + blockIdx.x; row < s1; row += gridDim.x)
+      for (int h = 0; h < heads; ++h) {
+        if (lane < C::D / 8) *reinterpret_cast<uint4*>(a.out + row * a.o_t + h * a.o_h + 8 * lane) = nan;
+        if (a.lse && lane == 0) a.lse[row * a.lse_t + h] = __uint_as_float(0x7FC00000u);
+      }
+  }
 }
 
 // A CTA's run of tiles, item after item; an item is one (sequence, block of rows, key head).
@@ -180,9 +201,10 @@ struct Walk {
     total = 0;
     long long items = 0;
     Seq own = {};                                              // of the first 32 sequences: read once
-    if (lane < a.batch) own = sequence<C>(a, lane);
+    bool over = false;
+    if (lane < a.batch) own = sequence<C>(a, lane, &over);
     for (int i = lane; i < a.batch; i += 32) {
-      const Seq q = i < 32 ? own : sequence<C>(a, i);
+      const Seq q = i < 32 ? own : sequence<C>(a, i, &over);
       total += (long long)q.tiles * q.blocks * a.kv_heads;
       items += q.tiles ? (long long)q.blocks * a.kv_heads : 0;
     }
@@ -191,6 +213,7 @@ struct Walk {
       total += __shfl_xor_sync(0xffffffffu, total, m);
       items += __shfl_xor_sync(0xffffffffu, items, m);
     }
+    if (__any_sync(0xffffffffu, over)) blank_rows<C>(a);
     const int grid = (int)gridDim.x;
     ctas = (int)min((long long)grid, (total + C::MIN_RUN - 1) / C::MIN_RUN);
     pad = 1;

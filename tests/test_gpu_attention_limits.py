@@ -46,3 +46,42 @@ def test_a_context_beyond_its_table_sees_the_table_and_costs_no_more(hk, group, 
     s.dev["table"] = s.dev["table"][:, :0]
     out, lse = s.run(out=torch.full_like(good, 7.0), lse=torch.full_like(glse, 7.0), workspace=ws)
     assert B.conqur_kv_status() == -11 and not out[:9].any() and torch.isneginf(lse[:9]).all() and (out[9:] == 7.0).all()
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+@pytest.mark.parametrize("hk,group,d", [(2, 2, 64), (1, 4, 128), (2, 10, 128), (1, 20, 64)])
+def test_tokens_behind_max_nodes_are_nan_and_told_of(hk, group, d, bits):
+    """A call whose max_nodes (1 unless given) is too small: no row of a sequence is left unwritten, and the rows that are computed are right."""
+    B, torch = _B(), _t()
+    s = Setup(102, [70] * 40 + [5], [1] * 39 + [5, 1], hk, group, d, 16, bits, kind="chain")
+    s.masks[39] = [1] * 5
+    s.mask[39:44] = 1
+    good, glse = (x.clone() for x in s.run(max_nodes=5))
+    for args in (dict(out=torch.full_like(good, 7.0), lse=torch.full_like(glse, 7.0)), dict(out=None, lse=None)):
+        out, lse = s.run(max_nodes=1, **args)
+        assert B.conqur_kv_status() == -11
+        assert torch.isnan(out[40:44]).all() and torch.isnan(lse[40:44]).all()
+        if args["out"] is not None:
+            out[40:44], lse[40:44] = good[40:44], glse[40:44]
+            s.check(out, lse)
+    # two at the most: the second of the long one is there, too
+    out, lse = s.run(max_nodes=2, out=torch.full_like(good, 7.0), lse=torch.full_like(glse, 7.0))
+    assert B.conqur_kv_status() == -11 and torch.isnan(out[41:44]).all() and torch.isnan(lse[41:44]).all()
+    out[41:44], lse[41:44] = good[41:44], glse[41:44]
+    s.check(out, lse)
+    # without lse, into strided rows: nothing beside them is touched
+    wide = torch.full((s.rows, hk * group + 1, d + 8), 7.0, device="cuda").bfloat16()
+    s.run(max_nodes=1, out=wide[:, 1:, :d])
+    assert B.conqur_kv_status() == -11 and torch.isnan(wide[40:44, 1:, :d]).all()
+    assert (wide[..., d:] == 7.0).all() and (wide[:, 0] == 7.0).all() and (wide[45:] == 7.0).all()
+    # thousands of tokens where one was meant, and spans that leave q: those sequences are left out
+    n = 3000
+    q = torch.randn(n, hk * group, d, device="cuda").bfloat16()
+    one = dict(contexts=s.dev["contexts"][:1], table=s.dev["table"][:1])
+    ws = B.attention_workspace(s.cache, group, 1)
+    out, lse = B.conqur_tree_attention(q, s.cache, torch.tensor([0, n], dtype=torch.int32, device="cuda"), workspace=ws, **one)
+    assert B.conqur_kv_status() == -11 and torch.isfinite(out[0]).all() and torch.isnan(out[1:]).all() and torch.isnan(lse[1:]).all()
+    for span in ([0, n + 1], [-1, n], [5, 3]):
+        o, l = torch.full_like(q, 7.0), torch.full_like(lse, 7.0)
+        B.conqur_tree_attention(q, s.cache, torch.tensor(span, dtype=torch.int32, device="cuda"), workspace=ws, out=o, lse=l, **one)
+        assert B.conqur_kv_status() == -11 and (o == 7.0).all() and (l == 7.0).all()
