@@ -607,7 +607,7 @@ int conqur_kv_status(void* cuda_stream);
  * place l % page_size of page table[b][l / page_size].  Drafted token i sees every position l < contexts[b] and those drafted tokens j
  * whose bit is set in its mask (a tree: itself and its ancestors); mask_dev NULL: j <= i (a chain; T_b = 1 is ordinary decoding).
  * Query head h reads key head h / group:
- *   s_l = scale q . k_l over the positions seen,  out = softmax(s) V,  lse = ln sum exp(s)     (nothing seen: out = 0, lse = -inf)
+ *   s_l = scale q . k_l over the positions seen,  out = softmax(s) V,  lse = ln sum exp(s)     (nothing seen, or only scores of -inf: out = 0, lse = -inf)
  * Arithmetic: products of bf16 values, exact in fp32 (4-bit codes enter as integers), sums, maxima and exponentials in fp32; a probability (bits 4: times its
  * token's value step) enters the product with the values rounded to bf16.  bits 4: |q| < 2^31 and value steps < 2^28 (beyond, infinities appear).  The sums over positions are split over the GPU in a way that depends on
  * the lengths of all sequences of the call: the same call gives the same bits, another batch around a sequence may change last bits.

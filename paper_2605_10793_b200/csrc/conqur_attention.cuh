@@ -11,8 +11,9 @@
 //     fragments in registers, in an order of dimensions (and of output dimensions) that lets every lane read whole words of a token's row;
 //     a product does not depend on the order of what it sums over.
 //   - P^T goes from the accumulator layout of the first product to the operand layout of the second with movmatrix, two per eight rows.
-//   - The running maximum is only a bound: rows are rescaled when a score exceeds it by 2^8, one vote per 16 tokens instead of a
-//     reduction (P is rounded relatively, a common factor changes nothing).
+//   - The running maximum is only a bound: rows are rescaled when a score exceeds it by 2^8, one vote per 32 tokens instead of a
+//     reduction (P is rounded relatively, a common factor changes nothing).  It starts at the lowest finite number, not at -inf: a token whose score is
+//     -inf then has the weight 0 that it is due also where no other has been met.
 //   - The work, in tiles of tokens of one sequence, key head and block of rows, is laid end to end and cut into equal runs, one per
 //     resident CTA, whatever the lengths (Walk has the exception for few items).  A piece of work that is cut leaves its parts (accumulators, maximum, sum) in the workspace; the
 //     last CTA to finish one of its parts adds them up in their order.  No CTA waits for another.
@@ -132,6 +133,8 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+
+constexpr float ATTN_NO_BOUND = -3.4028234663852886e38f;       // before the first score
 
 // The drafted tokens and context of a sequence, and what its work comes to.
 struct Seq {
@@ -426,13 +429,13 @@ struct Acc {
       for (int t = 0; t < C::KS; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[n][t][i] = 0.f;
-      m[n][0] = m[n][1] = -INFINITY;
+      m[n][0] = m[n][1] = ATTN_NO_BOUND;
       l[n][0] = l[n][1] = 0.f;
       z[n][0] = z[n][1] = z[n][2] = z[n][3] = 0.f;
     }
   }
   // The factor that takes sums under bound `from` to bound `to` >= from.
-  static __device__ __forceinline__ float shrink(float from, float to) { return to == -INFINITY ? 1.f : ex2(from - to); }
+  static __device__ __forceinline__ float shrink(float from, float to) { return ex2(from - to); }
   __device__ __forceinline__ void rescale(int n, int j, float to) {
     const float f = shrink(m[n][j], to);
     m[n][j] = to;
@@ -641,7 +644,7 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
       for (int i = 0; i < 4; ++i) sc[u][n][i] += sd[n][i];
   }
 
-  // ---- exponents against the rows' bounds (none yet: -inf, so that the first scores exceed it)
+  // ---- exponents against the rows' bounds (none yet: any finite score is above it)
   float x[H][NT][4], top = -INFINITY;
   unsigned long long mask[NT][2];
   if (EDGE)
@@ -706,7 +709,6 @@ __device__ __forceinline__ void attn_tokens(const AttnArgs& a, Acc<C>& acc, uint
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p[i] = ex2(x[u][n][i]);
-        if (EDGE && sc[u][n][i] == -INFINITY) p[i] = 0.f;          // not seen (and the bound may be -inf still)
         acc.l[n][i & 1] += p[i];
         if (C::BITS == 4) {
           p[i] *= (i & 2) ? v1 : v0;
@@ -829,7 +831,7 @@ __device__ void attn_write(const AttnArgs& a, Acc<C>& acc, const Seq& s, int ite
       for (int k = 4; k < 32; k <<= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
       const int r = first + n * 8 + 2 * c + j;
       if (r >= rows) continue;
-      const bool none = acc.m[n][j] == -INFINITY && l == 0.f;         // nothing seen
+      const bool none = l == 0.f;                                     // nothing seen, or nothing but scores of -inf
       const float inv = none ? 0.f : 1.f / l;
       const int node = r / a.group, h = head * a.group + r - node * a.group;
       const long long row = s.start + node;
@@ -852,7 +854,7 @@ __device__ void attn_write(const AttnArgs& a, Acc<C>& acc, const Seq& s, int ite
           o[t * 16 + g + 8] = __float2bfloat16_rn(acc.o[n][t][2 + j] * inv);
         }
       }
-      if (a.lse && g == 0) a.lse[row * a.lse_t + h] = none ? -INFINITY : (acc.m[n][j] == -INFINITY ? 0.f : acc.m[n][j]) * 0.6931471805599453f + logf(l);
+      if (a.lse && g == 0) a.lse[row * a.lse_t + h] = none ? -INFINITY : acc.m[n][j] * 0.6931471805599453f + logf(l);
     }
 }
 

@@ -85,3 +85,33 @@ def test_tokens_behind_max_nodes_are_nan_and_told_of(hk, group, d, bits):
         o, l = torch.full_like(q, 7.0), torch.full_like(lse, 7.0)
         B.conqur_tree_attention(q, s.cache, torch.tensor(span, dtype=torch.int32, device="cuda"), workspace=ws, out=o, lse=l, **one)
         assert B.conqur_kv_status() == -11 and (o == 7.0).all() and (l == 7.0).all()
+
+
+@pytest.mark.parametrize("hk,group,nodes", [(2, 1, 1), (2, 4, 1), (1, 4, 3), (2, 8, 2), (2, 8, 4), (1, 16, 20)])
+@pytest.mark.parametrize("context,low", [(0, (0, 1)), (90, (0, 64)), (300, (0, 300)), (300, (32, 64)), (9000, (0, 8990)), (9000, (100, 9000))])
+def test_scores_of_minus_infinity_weigh_nothing(context, low, hk, group, nodes):
+    """Keys with an element of -inf that every query meets with a positive one: weight 0, also where a warp, a stream or a part of an item has met no other."""
+    B, torch = _B(), _t()
+    d, page = 128, 32
+    s = Setup(103, [context, 33], [nodes, 1], hk, group, d, page, 16, kind="chain")
+    s.q[..., 5] = np.abs(s.q[..., 5]) + 0.5
+    s.q = K.bf16(s.q)
+    s.dev["q"] = torch.from_numpy(s.q.astype(np.float32)).cuda().bfloat16()
+    at = torch.arange(*low, device="cuda")
+    k, v = (torch.from_numpy(x[0][low[0]:low[1]].astype(np.float32)).cuda().bfloat16() for x in (s.k, s.v))
+    k[..., 5] = float("-inf")
+    B.conqur_kv_append(s.cache, k, v, s.dev["table"][0].long()[at // page] * page + at % page)
+    out, lse = s.run()
+    assert B.conqur_kv_status() == 0
+    seen = np.ones((nodes, context + nodes), bool)
+    for i in range(nodes):
+        seen[i, context + i + 1:] = False
+    seen[:, low[0]:low[1]] = False                           # what weighs nothing might as well not be seen
+    for h in range(hk * group):
+        want, wl, mass, size = K.attend(s.q[:nodes, h], s.k[0][:, h // group], s.v[0][:, h // group], seen, d ** -0.5)
+        delta = 2.0 ** -18 * size
+        bound = (2.0 ** -8 + 2 * delta[:, None] + 2.0 ** -19) * mass + 2.0 ** -8 * np.abs(want) + 1e-30
+        assert (np.abs(out[:nodes, h].float().cpu().numpy() - want) <= bound).all(), h
+        got, none = lse[:nodes, h].cpu().numpy().astype(np.float64), np.isneginf(wl)
+        assert np.array_equal(np.isneginf(got), none)
+        assert (np.abs(got[~none] - wl[~none]) <= (delta + 2.0 ** -20 * np.abs(wl) + 2.0 ** -13)[~none]).all()
