@@ -23,6 +23,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 
 #include "../../include/conqur.h"
@@ -55,6 +56,7 @@ struct HeadsArgs {
 enum { MODE_ROPE = 0, MODE_NORM = 1, MODE_GRAD = 2 };
 constexpr int HEADS_THREADS = 128;
 constexpr int HEADS_WARPS = HEADS_THREADS / 32;
+constexpr float NORM_DOWN = 8.470329472543003e-22f;      // 2^-70
 constexpr int GRAD_BLOCKS_MAX = 1184;      // 8 per SM: rows of partial weight gradients in the scratch
 
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
@@ -239,6 +241,24 @@ __device__ __forceinline__ void row_hadamard(Pairs& x, int l) {
   }
 }
 
+// Rows whose squares add up to more than an fp32 holds (rare; the whole warp comes here): scaled by 2^-70, beside which eps is nothing, they have a norm again.
+// Returns the factor 1 / sqrt(mean x^2 + eps) that goes with what is left in x.
+template <int L>
+__device__ __forceinline__ float row_down(Pairs& x, float square, int l, int lane, float inv_d, float eps) {
+  const bool big = !(square <= FLT_MAX);
+  const f2 down = mk2(big ? NORM_DOWN : 1.f);
+  f2 ss = 0ull;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x.a[i] = mul2(x.a[i], down);
+    x.b[i] = mul2(x.b[i], down);
+    ss = fma2(x.a[i], x.a[i], ss);
+    ss = fma2(x.b[i], x.b[i], ss);
+  }
+  const float small = row_sum<L>(sum2(ss), l, lane);
+  return rsqrtf(fmaf(big ? small : square, inv_d, big ? 0.f : eps));
+}
+
 // Pairs that do not turn keep to their own element (a sine of 0 would let what is not finite over); their cosine is the scale.
 template <bool HALF>
 __device__ __forceinline__ void row_spin(Pairs& x, const f2 (&c)[4], const f2 (&s)[4], uint32_t turned) {
@@ -414,7 +434,9 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 6 : 5) heads_k
         for (int i = 1; i < 4; ++i) ss = fma2(x.a[i], x.a[i], ss);
 #pragma unroll
         for (int i = 0; i < 4; ++i) ss = fma2(x.b[i], x.b[i], ss);
-        f *= rsqrtf(fmaf(row_sum<L>(sum2(ss), l, lane), 1.f / D, a.eps));
+        const float square = row_sum<L>(sum2(ss), l, lane);
+        if (__any_sync(0xffffffffu, h < heads && !(square <= FLT_MAX))) f *= row_down<L>(x, square, l, lane, 1.f / D, a.eps);
+        else f *= rsqrtf(fmaf(square, 1.f / D, a.eps));
       }
       if (before) row_hadamard<L>(x, l);
       if (NORM) {
@@ -524,6 +546,19 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 4 : 3) heads_g
       } else if (token + stride < a.n) {
         begin(token + stride);
       }
+      f2 ss = mul2(x.a[0], x.a[0]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i) ss = fma2(x.a[i], x.a[i], ss);
+        ss = fma2(x.b[i], x.b[i], ss);
+      }
+      const float square = row_sum<L>(sum2(ss), l, lane);
+      float r = rsqrtf(fmaf(square, 1.f / D, a.eps));
+      float down = 1.f;
+      if (__any_sync(0xffffffffu, now && !(square <= FLT_MAX))) {
+        r = row_down<L>(x, square, l, lane, 1.f / D, a.eps);
+        down = square <= FLT_MAX ? 1.f : NORM_DOWN;
+      }
       if (a.hadamard) row_hadamard<L>(y, l);
       row_spin<HALF>(y, c, s, q.turned);
       Piece<float> w0, w1;                                     // (shared memory: sixteen registers less)
@@ -531,29 +566,26 @@ __global__ void __launch_bounds__(HEADS_THREADS, sizeof(T) == 2 ? 4 : 3) heads_g
       w1.load(weight + q.p1);
       w0.get(v); w1.get(v + 8);
       const Pairs w = pairs_of<HALF>(v);
-      f2 ss = mul2(x.a[0], x.a[0]), sx = 0ull;
+      f2 sx = 0ull;
       Pairs wy;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (i) ss = fma2(x.a[i], x.a[i], ss);
-        ss = fma2(x.b[i], x.b[i], ss);
         wy.a[i] = mul2(w.a[i], y.a[i]);
         wy.b[i] = mul2(w.b[i], y.b[i]);
         sx = fma2(wy.a[i], x.a[i], sx);
         sx = fma2(wy.b[i], x.b[i], sx);
       }
-      const float r = rsqrtf(fmaf(row_sum<L>(sum2(ss), l, lane), 1.f / D, a.eps));
-      const float k = -row_sum<L>(sum2(sx), l, lane) * (1.f / D) * r * r;
+      const float k = -row_sum<L>(sum2(sx), l, lane) * (1.f / D) * r * (r * down);
       if (now) {
-        const f2 r2 = mk2(r), k2 = mk2(k);
+        const f2 r2 = mk2(r), d2 = mk2(r * down), k2 = mk2(k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           x.a[i] = mul2(x.a[i], r2);
           x.b[i] = mul2(x.b[i], r2);
           dw.a[i] = fma2(y.a[i], x.a[i], dw.a[i]);
           dw.b[i] = fma2(y.b[i], x.b[i], dw.b[i]);
-          y.a[i] = fma2(x.a[i], k2, mul2(wy.a[i], r2));
-          y.b[i] = fma2(x.b[i], k2, mul2(wy.b[i], r2));
+          y.a[i] = fma2(x.a[i], k2, mul2(wy.a[i], d2));
+          y.b[i] = fma2(x.b[i], k2, mul2(wy.b[i], d2));
         }
         pairs_to<HALF>(y, v);
         Piece<T>::store(op + q.p0, v);
@@ -677,6 +709,21 @@ __global__ void __launch_bounds__(HEADS_THREADS) heads_general_kernel(const Head
           x[j] = e < D ? load1(xp + e) : 0.f;
           ss = fmaf(x[j], x[j], ss);
         }
+        float down = 1.f;                                      // as in row_down
+        if (MODE != MODE_ROPE) {
+          ss = warp_sum(ss);
+          if (!(ss <= FLT_MAX)) {
+            down = NORM_DOWN;
+            ss = 0.f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              x[j] *= down;
+              ss = fmaf(x[j], x[j], ss);
+            }
+            ss = warp_sum(ss);
+          }
+        }
+        const float r = MODE == MODE_ROPE ? 1.f : 1.f / sqrtf(ss * inv + a.eps * (down * down));
         if (MODE == MODE_GRAD) {
           const T* yp = static_cast<const T*>(g.grad) + b * g.grad_b + t * g.grad_t + h * g.grad_h;
           for (int e = lane; e < D; e += 32) buf[e] = load1(yp + e);
@@ -689,9 +736,7 @@ __global__ void __launch_bounds__(HEADS_THREADS) heads_general_kernel(const Head
             const int e = lane + 32 * j;
             if (e < D) sx = fmaf(load_weight(g.weight, a.weight_bf16, e) * buf[e], x[j], sx);
           }
-          ss = warp_sum(ss);
           sx = warp_sum(sx);
-          const float r = 1.f / sqrtf(ss * inv + a.eps);
           const float k = sx * inv * r * r;
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
@@ -699,14 +744,12 @@ __global__ void __launch_bounds__(HEADS_THREADS) heads_general_kernel(const Head
             if (e < D) {
               const float y = buf[e];
               dw[j] = fmaf(y, x[j] * r, dw[j]);
-              store1(op + e, r * fmaf(load_weight(g.weight, a.weight_bf16, e), y, -x[j] * k));
+              store1(op + e, r * down * fmaf(load_weight(g.weight, a.weight_bf16, e), y, -x[j] * k));
             }
           }
           __syncwarp();
           continue;
         }
-        float r = 1.f;
-        if (MODE == MODE_NORM) r = 1.f / sqrtf(warp_sum(ss) * inv + a.eps);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int e = lane + 32 * j;
