@@ -629,7 +629,7 @@ typedef struct {
   int64_t  q_token_stride, q_head_stride;
   void*    out_dev;         /* device bf16, 16-byte aligned; strides multiples of 8 elements; must not overlap q */
   int64_t  out_token_stride, out_head_stride;
-  float*   lse_dev;         /* device, or NULL: row i, head h at [i lse_token_stride + h] */
+  float*   lse_dev;         /* device, or NULL: row i, head h at [i lse_token_stride + h]; the stride is at least the query heads */
   int64_t  lse_token_stride;
   const int32_t* starts_dev;      /* batch + 1, not decreasing */
   const int32_t* contexts_dev;    /* batch */

@@ -469,7 +469,9 @@ int tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* c, cons
   if (((reinterpret_cast<uintptr_t>(c->q_dev) | reinterpret_cast<uintptr_t>(c->out_dev)) & 15) ||
       ((c->q_token_stride | c->q_head_stride | c->out_token_stride | c->out_head_stride) & 7))
     return CONQUR_ERR_INVALID_ARG;
-  if ((c->rows > 1 && c->out_token_stride == 0) || ((int64_t)cache->kv_heads * c->group > 1 && c->out_head_stride == 0)) return CONQUR_ERR_INVALID_ARG;
+  const int64_t heads = (int64_t)cache->kv_heads * c->group;
+  if (c->lse_dev && c->rows > 1 && c->lse_token_stride < heads && c->lse_token_stride > -heads) return CONQUR_ERR_INVALID_ARG;
+  if ((c->rows > 1 && c->out_token_stride == 0) || (heads > 1 && c->out_head_stride == 0)) return CONQUR_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(c->starts_dev) | reinterpret_cast<uintptr_t>(c->contexts_dev) | reinterpret_cast<uintptr_t>(c->table_dev) |
        reinterpret_cast<uintptr_t>(c->lse_dev)) & 3)
     return CONQUR_ERR_INVALID_ARG;
