@@ -14,5 +14,5 @@ def test_what_is_not_a_wait_is_refused(B, block, site, tile):  # noqa: F811
 def test_few_rows_have_no_such_waits(B):  # noqa: F811
     lib = B.load()
     assert lib.conqur_debug_tree_attention(C.byref(_cache(B)), _tree(B, group=4, nodes=4), 0, 1, 0, None) == -10
-    assert lib.conqur_debug_tree_attention(C.byref(_cache(B)), _tree(B, group=8, nodes=8, ws=0), 0, 1, 0, None) == -1
-    assert lib.conqur_debug_tree_attention(C.byref(_cache(B)), _tree(B, group=8, nodes=8, wsb=1), 0, 1, 0, None) == -2
+    assert lib.conqur_debug_tree_attention(C.byref(_cache(B)), _tree(B, group=8, nodes=8, lse_t=64, ws=0), 0, 1, 0, None) == -1
+    assert lib.conqur_debug_tree_attention(C.byref(_cache(B)), _tree(B, group=8, nodes=8, lse_t=64, wsb=1), 0, 1, 0, None) == -2
