@@ -479,8 +479,9 @@ int conqur_hadamard_status(void* cuda_stream);
  *   R_3        x <- x H / sqrt(head_dim) with CONQUR_HEADS_HADAMARD (H as in conqur_hadamard_rows)
  * CONQUR_HEADS_INVERSE (conqur_rope_heads) applies the transposed map, R_3 first and the angles negated (the amplitude m is not
  * inverted): the backward pass of the forward call, and for m = 1 its inverse.
- * Arithmetic is fp32, rounded once to the storage type; angles are formed in 64-bit fixed point (turns modulo 1, exact
- * products), so that they stay accurate at any int64 position.
+ * Arithmetic is fp32, rounded once to the storage type.  An angle is the position times a 64-bit fraction of a turn, exactly, modulo 1: off by at
+ * most |position| 2^-64 + 2^-26 of a turn, the same for every position up to 2^36 and a millionth of a turn at 2^44.  R_3 adds up head_dim
+ * elements before it scales: without a norm rows of 2^127 / head_dim and more may overflow.
  */
 enum { CONQUR_ROPE_HALF = 0, CONQUR_ROPE_INTERLEAVED = 1 };
 /* frequencies f_i = theta^(-2i/rotary_dim), i < rotary_dim/2, and how a context longer than the trained one rescales them:

@@ -12,7 +12,7 @@
 //     layout, so that a rotation is five packed operations for two pairs; a norm's factor comes last, where R_3's 1 / sqrt(d) is, and its weights lie in shared
 //     memory (in registers they would cost a quarter of the warps).
 //   - Angles: the table holds each frequency in turns per position as a 64-bit binary fraction.  position * fraction modulo 2^64 is the
-//     exact turn modulo 1 (one 64-bit product, no range reduction, any position), its top 32 bits go to sincospif.
+//     turn modulo 1 (one 64-bit product, no range reduction; the fraction's own rounding leaves position * 2^-64), its top 32 bits go to sincospif.
 //   - Lanes with the same place in their rows need the same angles: each computes its share of them and they hand them round.
 // Measured, heads of 128 in bf16: rotation and R_3 of 16384 tokens of 32 + 8 heads 65 us (5.2 TB/s of 6.6); norm and rotation of 8192 tokens 36 us (4.7 TB/s: 20
 // warps an SM, 2.3 waves of blocks), its backward pass 53 us (4.8 TB/s: 16 warps an SM, a row of either input in flight each); one token or some dozen: 2.5

@@ -46,3 +46,61 @@ def test_rows_whose_squares_pass_an_fp32(d, r, layout, r3, dtype):
     for i in range(2):
         same = (scale[i] == 1.0)[..., 0]
         assert torch.equal(y[i][same], y1[i][same]) and torch.equal(grads[i][same], g1[i][same])
+
+
+def _turns(r, theta=10000.0, scaling="none", factor=1.0, low=0.0, high=0.0, original=0):
+    """The frequencies in turns per position, to 50 digits (amplitudes aside)."""
+    from decimal import ROUND_CEILING, ROUND_FLOOR, Decimal as D, getcontext
+    getcontext().prec = 60
+    tau = 2 * D("3.14159265358979323846264338327950288419716939937510582097494459")
+    base, factor, out = D(theta).ln(), D(factor), []
+    if scaling == "ntk":
+        base += factor.ln() * r / (r - 2)
+    for i in range(r // 2):
+        f = (-base * 2 * i / r).exp()
+        if scaling == "linear":
+            f /= factor
+        elif scaling == "bands":
+            keep = min(max((D(original) * f / tau - D(low)) / (D(high) - D(low)), D(0)), D(1))
+            f *= keep + (1 - keep) / factor
+        elif scaling == "ramp":
+            dim = lambda u: r * (D(original) / (tau * D(u))).ln() / (2 * base)       # noqa: E731
+            a = max(dim(high).to_integral_value(ROUND_FLOOR), D(0))
+            b = min(dim(low).to_integral_value(ROUND_CEILING), D(r - 1))
+            g = min(max((i - a) / max(b - a, D("0.001")), D(0)), D(1))
+            f = f * (1 - g) + f / factor * g
+        out.append(f / tau)
+    return out
+
+
+@pytest.mark.parametrize("name", sorted(SCALINGS))
+@pytest.mark.parametrize("r", [4, 64, 128, 512])
+def test_frequencies_are_held_to_the_last_of_64_bits(r, name):
+    """A frequency's 64-bit fraction of a turn is off by less than one unit (2^-64): what positions multiply.  Against 60-digit arithmetic."""
+    from decimal import Decimal as D
+    B = _B()
+    for theta in ([10000.0, 1e6] if name not in ("bands", "ramp") else [SCALINGS[name].get("theta", 10000.0)]):
+        kw = dict(SCALINGS[name], theta=theta)
+        words = [int(v) & (2 ** 64 - 1) for v in B.Rope(r, **kw).table[: r // 2].tolist()]
+        for w, f in zip(words, _turns(r, **kw)):
+            assert abs(D(w) - f * D(2) ** 64) < 1
+
+
+@pytest.mark.parametrize("name", ["none", "bands"])
+def test_far_positions_against_the_frequencies_of_the_definition(name):
+    """Angles are off by at most |position| 2^-64 + 2^-26 of a turn."""
+    from decimal import Decimal as D
+    B, torch = _B(), _t()
+    d = 128
+    rope = B.Rope(d, layout="half", **SCALINGS[name])
+    far = [0, 7, 200000, 2 ** 31 - 1, 2 ** 31 + 5, -2 ** 31 - 5, 2 ** 36 + 99, 2 ** 40 + 12345, -2 ** 40 - 7, 2 ** 44 + 1]
+    turns = [[p * f for f in _turns(d, **SCALINGS[name])] for p in far]
+    turn = np.array([[float(t - t.to_integral_value()) for t in row] for row in turns])
+    x = torch.randn(len(far), 2, d, device="cuda")
+    y, _ = B.conqur_rope_heads(x, None, torch.tensor(far, device="cuda"), rope)
+    c, s = np.cos(2 * np.pi * turn)[:, None], np.sin(2 * np.pi * turn)[:, None]
+    x64 = _np(x)
+    a, b = x64[..., : d // 2], x64[..., d // 2:]
+    want = np.concatenate((a * c - b * s, a * s + b * c), axis=-1)
+    word = 2 * np.pi * np.abs(np.array(far, dtype=np.float64))[:, None, None] * 2.0 ** -64
+    _within(_np(y), want, (2.0 ** -18 + word) * _norms(x64), "f32")
