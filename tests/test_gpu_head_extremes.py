@@ -104,3 +104,53 @@ def test_far_positions_against_the_frequencies_of_the_definition(name):
     want = np.concatenate((a * c - b * s, a * s + b * c), axis=-1)
     word = 2 * np.pi * np.abs(np.array(far, dtype=np.float64))[:, None, None] * 2.0 ** -64
     _within(_np(y), want, (2.0 ** -18 + word) * _norms(x64), "f32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,r,layout", [(128, 64, "half"), (80, 40, "interleaved"), (96, 24, "half")])
+def test_backward_in_place_and_with_a_scratch_of_the_caller(d, r, layout, dtype):
+    """The gradients of the inputs may take the place of those of the outputs (or of the inputs), inside a wider buffer; the scratch may hold anything."""
+    B, torch = _B(), _t()
+    rope = B.Rope(r, layout=layout)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n, hq, hk = 301, 6, 2
+    x = torch.randn(n, hq + hk + 1, d, device="cuda").to(dt)
+    g = torch.randn(n, hq + hk + 1, d, device="cuda").to(dt)
+    split = lambda t: (t[:, :hq], t[:, hq:hq + hk])                            # noqa: E731
+    w = [(1.0 + 0.3 * torch.randn(d, device="cuda")).to(dt) for _ in range(2)]
+    pos = torch.arange(n, device="cuda") + 17
+    want = B.conqur_norm_rope_heads_backward(*split(g), *split(x), *w, pos, rope, hadamard=d == 128)
+    scratch = torch.full((B.load().conqur_norm_rope_backward_scratch_bytes(d),), 0xFF, dtype=torch.uint8, device="cuda")
+    for own in (g.clone(), None):
+        grads, heads = (own, x) if own is not None else (g, x.clone())
+        into = grads if own is not None else heads
+        got = B.conqur_norm_rope_heads_backward(*split(grads), *split(heads), *w, pos, rope, hadamard=d == 128, out=split(into), scratch=scratch)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert got[0].data_ptr() == into.data_ptr() and torch.equal(into[:, -1], (g if own is not None else x)[:, -1])
+    with pytest.raises(B.ConqurError):
+        B.conqur_norm_rope_heads_backward(*split(g), *split(x), *w, pos, rope, scratch=scratch[:-256])
+    with pytest.raises(B.ConqurError):
+        B.conqur_norm_rope_heads_backward(*split(g), *split(x), *w, pos, rope, scratch=torch.empty(scratch.numel() + 64, dtype=torch.uint8, device="cuda")[8:])
+
+
+def test_backward_past_32_bit_offsets():
+    """Element offsets beyond 2^32: the first and last tokens' gradients are those of small copies; the weight gradients are both ends' sums."""
+    B, torch = _B(), _t()
+    d, h = 128, 8
+    n = (2 ** 32) // (h * d) + 300
+    x = torch.zeros(n, h, d, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros_like(x)
+    ends = (slice(0, 70), slice(n - 70, n))
+    for e in ends:
+        x[e].normal_()
+        g[e].normal_()
+    pos = torch.arange(n, device="cuda")
+    w = (1.0 + 0.3 * torch.randn(d, device="cuda")).bfloat16()
+    rope = B.Rope(d)
+    small = [B.conqur_norm_rope_heads_backward(g[e].clone(), None, x[e].clone(), None, w, None, pos[e].clone(), rope) for e in ends]
+    x64, g64 = (np.concatenate([_np(t[e]) for e in ends]) for t in (x, g))
+    rms = 1.0 / np.sqrt(np.mean(x64 * x64, axis=-1, keepdims=True) + 1e-6)
+    dq, _, dw, _ = B.conqur_norm_rope_heads_backward(g, None, x, None, w, None, pos, rope, out=(g, None))
+    assert all(torch.equal(dq[e], s[0]) for e, s in zip(ends, small)) and not dq[70:-70:1013].any().item()
+    bound = 2 * (2.0 ** -16 + 2.0 ** -18) * (np.abs(x64 * rms) * _norms(g64)).sum(axis=(0, 1))
+    _within(_np(dw), _np(small[0][2]) + _np(small[1][2]), bound, "f32")
