@@ -647,16 +647,17 @@ size_t conqur_tree_attention_workspace_bytes(const conqur_kv_cache* cache, int32
 int conqur_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* call, void* cuda_stream);
 
 /*
- * Test support: conqur_tree_attention for more than 16 rows a key head (group * max_nodes; others return CONQUR_ERR_UNSUPPORTED), in which thread
- * block `block` waits at `site` of the tile `tile` of its run (64 tokens each, from 0) for what never comes, and waits end after about 5 ms.  Where the
- * block gets that far, CONQUR_ERR_TIMEOUT is latched and the context of the process stays usable.
+ * Test support: conqur_tree_attention for more than 16 rows a key head (group * max_nodes; others return CONQUR_ERR_UNSUPPORTED), in which one
+ * barrier of thread block `block`, number `index` of those of `site`, never completes, and the block gives up after about 5 ms.  A block takes the tiles of its
+ * run (64 tokens each) in four stages and two streams, in turn.  Where somebody waits for that barrier CONQUR_ERR_TIMEOUT is latched; the context of
+ * the process stays usable.
  */
-enum { CONQUR_TREE_WAIT_STAGE = 1,          /* a free stage, by the warps that bring keys and values */
-       CONQUR_TREE_WAIT_TILE = 2,           /* a tile's keys and values, by the warp that issues products */
-       CONQUR_TREE_WAIT_PROBABILITIES = 3,  /* a tile's probabilities, by the same */
-       CONQUR_TREE_WAIT_SCORES = 4,         /* a tile's scores, by the warps of the rows */
-       CONQUR_TREE_WAIT_OUTPUT = 5 };       /* a stream's last product of an item, by the same (tile: the one that product is of) */
-int conqur_debug_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* call, int32_t block, int32_t site, int32_t tile, void* cuda_stream);
+enum { CONQUR_TREE_WAIT_STAGE = 1,          /* index 0 .. 3: a stage is free again (by the warps that bring the tile four further on) */
+       CONQUR_TREE_WAIT_TILE = 2,           /* 0 .. 3: a stage's keys and values are there */
+       CONQUR_TREE_WAIT_PROBABILITIES = 3,  /* 0, 1: a stream's probabilities are (by the warp that issues products) */
+       CONQUR_TREE_WAIT_SCORES = 4,         /* 0, 1: a stream's scores are (by the warps of the rows) */
+       CONQUR_TREE_WAIT_OUTPUT = 5 };       /* 0, 1: a stream's product with the values is complete (by the same, at its next tile or at the item's end) */
+int conqur_debug_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* call, int32_t block, int32_t site, int32_t index, void* cuda_stream);
 
 const char* conqur_strerror(int status);
 

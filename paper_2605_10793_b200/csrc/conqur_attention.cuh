@@ -39,9 +39,8 @@ struct AttnArgs {
   unsigned* counters;                // one per CTA, for the item that its run ends in the middle of: parts finished, wraps to 0
   float* parts;                      // two slots per CTA
   int* flags;
-  // conqur_attention_tc.cuh: cycles that a wait between the warps lasts at most, and (test support) the one wait that waits for what never comes
-  long long wait_limit;
-  int lose_block, lose_site, lose_tile;
+  // conqur_attention_tc.cuh, test support: the barrier of one CTA that expects one arrival more than it gets, a CONQUR_TREE_WAIT_* and its number
+  int lose_block, lose_site, lose_index;
 };
 
 enum { KV_FLAG_BAD_INDEX = 1, KV_FLAG_TIMEOUT = 2 };

@@ -21,6 +21,7 @@ namespace conqur {
 namespace kv {
 
 enum { BAR_ITEM = 5 };
+constexpr long long TREE_LOST_LIMIT = 10000000ll;              // some 5 ms
 
 template <int BITS_, int D_>
 struct TreeCfg {
@@ -40,13 +41,14 @@ struct TreeCfg {
 template <typename C>
 struct TreeAux {
   uint64_t full[C::STAGES], empty[C::STAGES], scored[2], read[2], ready[2], done[2];   // tile brought, free again; S complete, read; P written; P V complete
-  uint64_t drained, never;                                     // all products of the CTA complete; test support: nothing arrives here
-  float kstep[C::STAGES][64], vstep[C::STAGES][64];
+  uint64_t drained;                                            // all products of the CTA complete
+  alignas(16) float kstep[C::STAGES][64];                      // (read four at a time)
+  alignas(16) float vstep[C::STAGES][64];
   uint32_t bad[C::STAGES][2];                                  // tokens of a tile whose page could not be read
   float bound[2][128], sum[2][128];                            // of the two streams
   Walk<C> w;
   uint32_t tmem;
-  int abort_flag, last;
+  int abort_flag, ended, last;
   int odd;                                                     // some value or step of a drafted token was not finite (never taken back: it only asks for a look)
 };
 
@@ -157,15 +159,6 @@ __device__ __forceinline__ bool bar_any(int bar, int threads, bool mine) {
       : "r"(bar), "r"(threads), "r"((uint32_t)mine)
       : "memory");
   return any != 0u;
-}
-// The bounded wait of a whole warp; `site` (CONQUR_TREE_WAIT_*) and the tile's number in the CTA name it.
-template <typename C>
-__device__ __forceinline__ bool tree_wait(const AttnArgs& a, TreeAux<C>* aux, int site, int tile, uint64_t* bar, uint32_t parity) {
-  if (tile == a.lose_tile && site == a.lose_site && (int)blockIdx.x == a.lose_block) {
-    bar = &aux->never;
-    parity = 0u;
-  }
-  return __all_sync(0xffffffffu, tc_wait(bar, parity, &aux->abort_flag, a.wait_limit));
 }
 
 // ---- warps 8-11: a thread takes a token's 64 dimensions of one plane, of keys and values (D = 64: threads 0-63 the keys, 64-127 the values)
@@ -337,7 +330,6 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
   volatile int* abort_flag = &aux->abort_flag;
   const uint32_t tmem = aux->tmem, tO = tmem + C::T_O, tQ = tmem + C::T_Q, tP = tmem + C::T_P;
   Walk<C> w = aux->w;
-  bool issued = false;                                         // products: there are some that `drained` has to be asked about
   int cnt = 0;                                                 // tiles so far: stream and buffers cnt & 1, phase (cnt >> 1) & 1; stage cnt % S
   bool head_of_run = true, more = w.left > 0;
 
@@ -390,7 +382,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       int slot = 0;
       for (int i = i0; i < tiles; i += 2) {
         const int n = cnt + i, st = n % S;
-        if (!tree_wait<C>(a, aux, CONQUR_TREE_WAIT_STAGE, n, &aux->empty[st], ((uint32_t)(n / S) & 1u) ^ 1u)) break;
+        if (!tc_wait_warp(&aux->empty[st], ((uint32_t)(n / S) & 1u) ^ 1u, abort_flag)) break;
         uint8_t* mem = sT + st * STAGE;
         if (C::BITS == 16) {
           in.now[0] = in.next[0];
@@ -435,14 +427,13 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       const uint32_t t0 = ptx::smem_u32(sT);
       auto scores = [&](int n) {
         const int st = n % S;
-        if (!tree_wait<C>(a, aux, CONQUR_TREE_WAIT_TILE, n, &aux->full[st], (uint32_t)(n / S) & 1u)) return false;
+        if (!tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag)) return false;
         ptx::tc_fence_after();
         const uint32_t k0 = t0 + st * STAGE;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
           umma_from_tmem(leader, tmem + (n & 1) * 64, tQ + j * 8, tc_smem_desc(k0 + (j >> 2) * 8192 + (j & 3) * 32, 16, 1024), id_s, j > 0 ? 1u : 0u);
         ptx::umma_commit_by<false>(leader, ptx::smem_u32(&aux->scored[n & 1]));
-        issued = true;
         return true;
       };
       ok = scores(cnt) && (tiles < 2 || scores(cnt + 1));
@@ -456,13 +447,13 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
             ptx::tc_fence_after();
             if (!(ok = scores(n + 2))) break;
             next = true;
-          } else if (__any_sync(0xffffffffu, *abort_flag || clock64() - since > a.wait_limit)) {
+          } else if (__any_sync(0xffffffffu, *abort_flag || clock64() - since > TC_WAIT_LIMIT)) {
             *abort_flag = 1;
             ok = false;
             break;
           }
         }
-        if (!(ok = ok && tree_wait<C>(a, aux, CONQUR_TREE_WAIT_PROBABILITIES, n, &aux->ready[buf], (n >> 1) & 1))) break;
+        if (!(ok = ok && tc_wait_warp(&aux->ready[buf], (n >> 1) & 1, abort_flag))) break;
         ptx::tc_fence_after();
         const uint32_t v0 = t0 + (n % S) * STAGE + C::T_BYTES;
 #pragma unroll
@@ -482,9 +473,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
       for (int i = i0; i < tiles; i += 2) {
         const int n = cnt + i, st = n % S, first = (w.tile + i) * ATTN_UNIT;
         // (the steps come with the tile, the scores with its product)
-        if (!(ok = tree_wait<C>(a, aux, 0, n, &aux->full[st], (uint32_t)(n / S) & 1u) &&
-                   tree_wait<C>(a, aux, CONQUR_TREE_WAIT_SCORES, n, &aux->scored[buf], (n >> 1) & 1)))
-          break;
+        if (!(ok = tc_wait_warp(&aux->full[st], (uint32_t)(n / S) & 1u, abort_flag) && tc_wait_warp(&aux->scored[buf], (n >> 1) & 1, abort_flag))) break;
         ptx::tc_fence_after();
         const uint32_t tS = tmem + lanes + buf * 64;
         const unsigned long long bad = (unsigned long long)aux->bad[st][0] | ((unsigned long long)aux->bad[st][1] << 32);
@@ -529,7 +518,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         ptx::tc_fence_before();
         ptx::mbar_arrive(&aux->read[buf]);
         // P and O of the stream's tile before
-        if (!(ok = tree_wait<C>(a, aux, 0, n, &aux->done[buf], ((n >> 1) & 1) ^ 1))) break;
+        if (!(ok = tc_wait_warp(&aux->done[buf], ((n >> 1) & 1) ^ 1, abort_flag))) break;
         ptx::tc_fence_after();
         if (raise) {
           l *= f;
@@ -572,7 +561,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
         ptx::mbar_arrive(&aux->ready[buf]);
       }
       const int mine = tiles > i0 ? (tiles - 1 - i0) / 2 : -1, last = cnt + i0 + 2 * mine;      // the stream's last tile of the item
-      if (ok && mine >= 0) ok = tree_wait<C>(a, aux, CONQUR_TREE_WAIT_OUTPUT, last, &aux->done[buf], (last >> 1) & 1);
+      if (ok && mine >= 0) ok = tc_wait_warp(&aux->done[buf], (last >> 1) & 1, abort_flag);
       ptx::tc_fence_after();
       aux->bound[buf][r] = m;
       aux->sum[buf][r] = l;
@@ -712,7 +701,7 @@ __device__ __forceinline__ void tree_role(const AttnArgs& a, TreeAux<C>* aux, ui
     head_of_run = false;
     more = w.next(a);
   }
-  if (ROLE == TREE_PRODUCTS && issued) {
+  if (ROLE == TREE_PRODUCTS && aux->w.left > 0) {
     // A wait that ran out leaves products under way: they end before TMEM, the tiles and the barriers they arrive on are given back.
     ptx::umma_commit_by<false>(ptx::elect_one(), ptx::smem_u32(&aux->drained));
     const long long since = clock64();
@@ -733,19 +722,19 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
   volatile int* abort_flag = &aux->abort_flag;
   if (tid == 0) {
+    auto lost = [&](int site, int i) { return (int)blockIdx.x == a.lose_block && site == a.lose_site && i == a.lose_index ? 1 : 0; };
     for (int i = 0; i < S; ++i) {
-      ptx::mbar_init(&aux->full[i], 128);
-      ptx::mbar_init(&aux->empty[i], 1);
+      ptx::mbar_init(&aux->full[i], 128 + lost(CONQUR_TREE_WAIT_TILE, i));
+      ptx::mbar_init(&aux->empty[i], 1 + lost(CONQUR_TREE_WAIT_STAGE, i));
     }
     for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(&aux->scored[i], 1);
+      ptx::mbar_init(&aux->scored[i], 1 + lost(CONQUR_TREE_WAIT_SCORES, i));
       ptx::mbar_init(&aux->read[i], 128);
-      ptx::mbar_init(&aux->ready[i], 128);
-      ptx::mbar_init(&aux->done[i], 1);
+      ptx::mbar_init(&aux->ready[i], 128 + lost(CONQUR_TREE_WAIT_PROBABILITIES, i));
+      ptx::mbar_init(&aux->done[i], 1 + lost(CONQUR_TREE_WAIT_OUTPUT, i));
     }
     ptx::mbar_init(&aux->drained, 1);
-    ptx::mbar_init(&aux->never, 1);
-    aux->abort_flag = aux->odd = 0;
+    aux->abort_flag = aux->ended = aux->odd = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async();
   }
@@ -771,7 +760,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) attn_tree_kernel(const AttnArgs
     tree_role<C, TREE_BRING>(a, aux, sT, sRaw, warp);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (warp == 16) tree_role<C, TREE_PRODUCTS>(a, aux, sT, sRaw, warp);
+    if (warp == 16) {
+      tree_role<C, TREE_PRODUCTS>(a, aux, sT, sRaw, warp);
+      aux->ended = 1;
+    } else if (a.lose_site && (int)blockIdx.x == a.lose_block) {
+      // test support: gives up in place of a wait of two seconds
+      const long long since = clock64();
+      while (!*reinterpret_cast<volatile int*>(&aux->ended) && !*abort_flag)
+        if (clock64() - since > TREE_LOST_LIMIT) *abort_flag = 1;
+    }
   }
   ptx::tc_fence_before();
   __syncthreads();

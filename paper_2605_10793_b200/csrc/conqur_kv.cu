@@ -458,7 +458,7 @@ extern "C" size_t conqur_tree_attention_workspace_bytes(const conqur_kv_cache* c
 namespace {
 
 // The wait that a test asks for (conqur_debug_tree_attention); site 0: none.
-struct LostWait { int block, site, tile; };
+struct LostWait { int block, site, index; };
 
 int tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* c, const LostWait& lost, void* cuda_stream) {
   if (!c || c->struct_size != sizeof(conqur_tree_call) || !attn_sizes_ok(cache, c->batch, c->group, c->max_nodes)) return CONQUR_ERR_INVALID_ARG;
@@ -494,8 +494,7 @@ int tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* c, cons
   a.lse = c->lse_dev; a.lse_t = c->lse_token_stride;
   a.starts = c->starts_dev; a.contexts = c->contexts_dev; a.table = c->table_dev; a.table_stride = c->table_stride;
   a.mask = reinterpret_cast<const unsigned long long*>(c->mask_dev);
-  a.wait_limit = lost.site ? 10000000ll : TC_WAIT_LIMIT;       // some 5 milliseconds, or two seconds
-  a.lose_block = lost.block; a.lose_site = lost.site; a.lose_tile = lost.site ? lost.tile : -1;
+  a.lose_block = lost.block; a.lose_site = lost.site; a.lose_index = lost.index;
   a.counters = static_cast<unsigned*>(c->workspace_dev);
   a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(c->workspace_dev) + ATTN_COUNTER_BYTES);
 
@@ -529,10 +528,10 @@ int tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* c, cons
 }  // namespace
 
 extern "C" int conqur_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* call, void* cuda_stream) {
-  return tree_attention(cache, call, LostWait{0, 0, -1}, cuda_stream);
+  return tree_attention(cache, call, LostWait{0, 0, 0}, cuda_stream);
 }
 
-extern "C" int conqur_debug_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* call, int32_t block, int32_t site, int32_t tile, void* cuda_stream) {
-  if (block < 0 || tile < 0 || site < CONQUR_TREE_WAIT_STAGE || site > CONQUR_TREE_WAIT_OUTPUT) return CONQUR_ERR_INVALID_ARG;
-  return tree_attention(cache, call, LostWait{block, site, tile}, cuda_stream);
+extern "C" int conqur_debug_tree_attention(const conqur_kv_cache* cache, const conqur_tree_call* call, int32_t block, int32_t site, int32_t index, void* cuda_stream) {
+  if (block < 0 || site < CONQUR_TREE_WAIT_STAGE || site > CONQUR_TREE_WAIT_OUTPUT || index < 0 || index >= (site <= CONQUR_TREE_WAIT_TILE ? 4 : 2)) return CONQUR_ERR_INVALID_ARG;
+  return tree_attention(cache, call, LostWait{block, site, index}, cuda_stream);
 }
