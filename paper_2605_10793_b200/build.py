@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libconqur.so")
 OBJ = os.path.join(PKG, "build")
 SOURCES = ["conqur.cu", "conqur_noalloc.cu", "conqur_heads.cu", "conqur_kv.cu"]
-HEADERS = ["conqur_internal.h", "conqur_simt.cuh", "conqur_tc.cuh", "conqur_tc_batched.cuh", "conqur_split_tc.cuh", "conqur_ns_cluster.cuh", "conqur_fold_tc.cuh", "conqur_aux.cuh", "conqur_hadamard_tc.cuh", "conqur_attention.cuh", "conqur_attention_tc.cuh", "ns_schedule.h",
+HEADERS = ["conqur_internal.h", "conqur_simt.cuh", "conqur_ptx.cuh", "conqur_tc.cuh", "conqur_tc_batched.cuh", "conqur_split_tc.cuh", "conqur_ns_cluster.cuh", "conqur_fold_tc.cuh", "conqur_aux.cuh", "conqur_hadamard_tc.cuh", "conqur_attention.cuh", "conqur_attention_tc.cuh", "ns_schedule.h",
            os.path.join("..", "..", "include", "conqur.h")]
 
 

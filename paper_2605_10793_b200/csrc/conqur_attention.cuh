@@ -20,7 +20,10 @@
 //   - A warp takes groups of 32 tokens of its own and brings them with asynchronous 16-byte copies into a ring of its own: no warp waits for another
 //     but the one that adds up an item's parts: the warps take turns at that, the others go on with the next item.
 #pragma once
-#include "conqur_tc.cuh"
+#include <cuda_bf16.h>
+
+#include "../../include/conqur.h"
+#include "conqur_ptx.cuh"
 
 namespace conqur {
 namespace kv {
