@@ -610,7 +610,8 @@ int conqur_kv_status(void* cuda_stream);
  * Query head h reads key head h / group:
  *   s_l = scale q . k_l over the positions seen,  out = softmax(s) V,  lse = ln sum exp(s)     (nothing seen, or only scores of -inf: out = 0, lse = -inf)
  * Arithmetic: products of bf16 values, exact in fp32 (4-bit codes enter as integers), sums, maxima and exponentials in fp32; a probability (bits 4: times its
- * token's value step) enters the product with the values rounded to bf16.  bits 4: |q| < 2^31 and value steps < 2^28 (beyond, infinities appear).  The sums over positions are split over the GPU in a way that depends on
+ * token's value step) enters the product with the values rounded to bf16.  bits 4: |q| < 2^31, value steps < 2^28, scale and scale times
+ * key steps < 2^90 (beyond, infinities appear).  The sums over positions are split over the GPU in a way that depends on
  * the lengths of all sequences of the call: the same call gives the same bits, another batch around a sequence may change last bits.
  * A page index outside the cache or a position outside the table is not seen and latches CONQUR_ERR_BAD_INDEX (as do a negative context,
  * more than max_nodes drafted tokens, and rows outside q).  Of a sequence with more than max_nodes drafted tokens those behind the first max_nodes get

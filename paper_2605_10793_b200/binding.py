@@ -532,7 +532,8 @@ def conqur_rope_heads(q, k, positions, rope: Optional[Rope], hadamard=False, inv
     (see include/conqur.h).
 
     q, k: fp32 / bf16 CUDA tensors (tokens, heads, d) or (batch, tokens, heads, d), any strides but the last; k may be None.
-    positions: int64 (tokens,) or (batch, tokens).  out: (q_out, k_out), which may be (q, k).  Returns (q_out, k_out)."""
+    positions: int64 (tokens,) or (batch, tokens).  out: (q_out, k_out), which may be (q, k).  Returns (q_out, k_out).  Nothing is recorded for
+    torch's backward pass, here and below: in training call the inverse (conqur_norm_rope_heads_backward after a norm) from a function of your own."""
     stream = _here(q)
     flags = (CONQUR_HEADS_HADAMARD if hadamard else 0) | (CONQUR_HEADS_INVERSE if inverse else 0)
     call, q_out, k_out = _heads_call(q, k, positions, rope, flags, 0.0, None, None, out)
@@ -652,7 +653,8 @@ def conqur_tree_attention(q, cache: KVCache, starts, contexts, table, mask=None,
     table (b, pages a sequence): int32.  mask: int64 (tokens,), bit j of a token's: it sees drafted token j of its sequence; None: a
     chain.  max_nodes: the most tokens a sequence has (at most 64); those of a sequence behind its first max_nodes get NaN and conqur_kv_status tells
     of it.  It also chooses the kernel (up to 16 rows max_nodes * q_heads / kv_heads, or more), so no larger than needed.  scale: 1 / sqrt(head_dim) by default.  out, lse (fp32 (tokens, q_heads)):
-    given or made here; rows that no sequence names stay as they are.  workspace: from attention_workspace; made here if None."""
+    given or made here; rows that no sequence names stay as they are.  workspace: from attention_workspace; made here if None.  Nothing is recorded for
+    torch's backward pass."""
     stream = _here(q)
     t, dev = _torch, cache._device
     n, heads, d = q.shape

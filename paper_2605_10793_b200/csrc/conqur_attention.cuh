@@ -4,12 +4,15 @@
 //   s_l = scale q . k_l,  o = sum_l 2^(s_l log2 e - m) v_l / sum_l 2^(s_l log2 e - m),  m a running bound of the row's scores
 //
 // This file: at most 16 rows a key head.  The cache is read once, so memory sets the pace; over 4-bit codes the unpacking of a byte into two operands comes
-// close to it.  Measured on one row of 8 key heads of 4 query heads each, 64 sequences of 8192: bf16 322 us (6.67 TB/s, a copy's rate), 4 bits 124 us (4.6 TB/s:
-// about 1.1 instructions a code at two thirds of the issue rate); one sequence of 200: 9 us, of which 3 are a launch.
+// close to it.  Measured on one row of 8 key heads of 4 query heads each, 64 sequences of 8192: bf16 325 us (6.6 TB/s, a copy's rate), 4 bits 123 us (4.6 TB/s:
+// about 1.1 instructions a code, 2.15 of 4 a cycle and the ALU 57 % busy: 16 warps an SM whose chains of score, exponential and product, and ends of items, do
+// not overlap any further); one sequence of 200: 9 us, of which 3 are a launch.
 //   - The tokens, not the rows, are the 16-row side of the warps' products (m16n8k16): S^T = K Q^T and O^T = V^T P^T.  Eight
 //     rows fill an instruction, and a fragment of K or V that was unpacked from codes is used for all rows of the warp.  The codes go from shared memory to the
 //     fragments in registers, in an order of dimensions (and of output dimensions) that lets every lane read whole words of a token's row;
 //     a product does not depend on the order of what it sums over.
+//   - P is rounded to bf16, the values' type, which is what the products take: 2^-8 of a probability at most, either way, so that an output is off by 1.9 to
+//     2.4e-3 of itself (root mean square) where rounding it alone makes 1.6 to 1.7e-3.
 //   - P^T goes from the accumulator layout of the first product to the operand layout of the second with movmatrix, two per eight rows.
 //   - The running maximum is only a bound: rows are rescaled when a score exceeds it by 2^8, one vote per 32 tokens instead of a
 //     reduction (P is rounded relatively, a common factor changes nothing).  It starts at the lowest finite number, not at -inf: a token whose score is

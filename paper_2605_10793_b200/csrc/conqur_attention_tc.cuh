@@ -11,9 +11,9 @@
 // zeros of rows that do not see them only among the drafted tokens; there they are left out of the product and added at the item's end.  Work is cut into runs and
 // parts are joined as in conqur_attention.cuh.  Every wait between the warps is bounded: when one runs out the CTA latches TIMEOUT,
 // leaves the item that it is at and all later ones unwritten, waits for its products under way and ends.
-// Floor: 8192 exponentials a tile at 16 a cycle are 512 cycles, and the products take as long.  Measured, 37 sequences of 6000, 8 key heads, 128 rows: 159 us over
-// 4 bits, about 1500 cycles a tile (a half-used issue rate: the chain score - exponential - product of two streams is what is left), 223 us over bf16 (two
-// thirds of it the cache's bytes).  Sixteen rows in the kernel of conqur_attention.cuh take 78 us there, 32 rows would take two passes of it: 155, and here 153.
+// Floor: 8192 exponentials a tile at 16 a cycle are 512 cycles, and the products take as long.  Measured, 37 sequences of 6000, 8 key heads, 128 rows: 161 us over
+// 4 bits, about 1500 cycles a tile (a half-used issue rate: the chain score - exponential - product of two streams is what is left), 222 to 226 us over bf16 (two
+// thirds of it the cache's bytes).  Sixteen rows in the kernel of conqur_attention.cuh take 79 us there, 32 rows would take two passes of it: 158, and here 155.
 #pragma once
 #include "conqur_attention.cuh"
 

@@ -14,11 +14,14 @@
 //   - Angles: the table holds each frequency in turns per position as a 64-bit binary fraction.  position * fraction modulo 2^64 is the
 //     turn modulo 1 (one 64-bit product, no range reduction; the fraction's own rounding leaves position * 2^-64), its top 32 bits go to sincospif.
 //   - Lanes with the same place in their rows need the same angles: each computes its share of them and they hand them round.
-// Measured, heads of 128 in bf16: rotation and R_3 of 16384 tokens of 32 + 8 heads 65 us (5.2 TB/s of 6.6); norm and rotation of 8192 tokens 36 us (4.7 TB/s: 20
-// warps an SM, 2.3 waves of blocks), its backward pass 53 us (4.8 TB/s: 16 warps an SM, a row of either input in flight each); one token or some dozen: 2.5
-// to 3.6 us, a launch.  Every lane computing its own angles: 69, 38 and 69 us.  Two warps a token, half of its heads each: 72, 36.6 and 77 us.
+// Measured in a graph of launches, heads of 128 in bf16: rotation of 16384 tokens of 32 + 8 heads 54 us (6.2 TB/s of 6.6), with R_3 65 us (5.1 TB/s: its
+// exchanges, 2.5 of 4 instructions a cycle and the load/store pipe half busy); norm and rotation of 8192 tokens 35 us (4.8 TB/s: 24 warps an SM, 2.3 waves of
+// blocks), its backward pass 54 us (4.6 TB/s: 16 warps an SM, a row of either input in flight each); some dozen tokens: 2.7 to 4 us, a launch.
+// Every lane computing its own angles: 69 (R_3), 38 and 69 us.  Two warps a token, half of its heads each: 72, 36.6 and 77 us.
+// Six blocks of four warps an SM leave 80 registers a thread (fp32: five blocks, 96): the normed kernels spill 92 to 172 bytes at that, the others up to 72.
 // Rows that do not fit that scheme (head_dim not a multiple of 16 or without an instance below, half-layout pairs that do not lie in
-// whole pieces, rows off 16-byte boundaries) take a kernel that keeps one row per warp in shared memory.
+// whole pieces, rows off 16-byte boundaries) take a kernel that keeps one row per warp in shared memory: 16384 tokens of 32 + 8 heads of 96, 24 of them
+// rotated in halves, 182 us for 38 of bytes.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
