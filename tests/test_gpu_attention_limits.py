@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("bits", [4, 16])
 @pytest.mark.parametrize("hk,group", [(2, 2), (1, 4), (2, 16)])
 def test_a_context_beyond_its_table_sees_the_table_and_costs_no_more(hk, group, bits):
-    """Positions without a place in the table are not seen, however many the context claims: the work is that of the table (2^24 tiles took seconds)."""
+    """Positions without a place in the table are not seen, however many the context claims: the work is that of the table, not of 2^24 tiles."""
     B, torch = _B(), _t()
     s = Setup(101, [204, 205, 12], [4, 3, 2], hk, group, 128, 16, bits)       # the first two fill their 13 pages, and so the table
     good, glse = (x.clone() for x in s.run())
