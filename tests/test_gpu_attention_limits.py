@@ -21,11 +21,14 @@ def test_a_context_beyond_its_table_sees_the_table_and_costs_no_more(hk, group, 
     ws = B.attention_workspace(s.cache, group, 4)
     for claim in (205, 300, 2 ** 30, 2 ** 31 - 1):
         s.dev["contexts"][0] = claim
-        torch.cuda.synchronize()
-        begin = time.perf_counter()
-        out, lse = s.run(out=torch.full_like(good, 7.0), lse=torch.full_like(glse, 7.0), workspace=ws)
-        assert B.conqur_kv_status() == -11
-        assert time.perf_counter() - begin < 0.2
+        times = []
+        for _ in range(3):                                   # (the best of three: the host may be busy)
+            torch.cuda.synchronize()
+            begin = time.perf_counter()
+            out, lse = s.run(out=torch.full_like(good, 7.0), lse=torch.full_like(glse, 7.0), workspace=ws)
+            assert B.conqur_kv_status() == -11
+            times.append(time.perf_counter() - begin)
+        assert min(times) < 0.1
         assert torch.equal(out[4:], good[4:]) and torch.equal(lse[4:], glse[4:])
         # its drafted tokens lie at `claim` and behind: those past position 207 have no place; the others see by their masks
         seen = np.zeros((4, 208), bool)
